@@ -104,7 +104,8 @@ const char* bcq_status_string(bcq_status s);
 
 /* ABI version, bumped on any signature change or addition (2: *_grouped entry points; 3: bcq_quantize_alternating; 4: AdamW entry points;
  * 5: decode layout; 6: bcq_linear_fwd_static;
- * 7: batched small-token calls; 8: bcq_prepare, bcq_batch_prepare; 9: bcq_linear_fwd_lut). */
+ * 7: batched small-token calls; 8: bcq_prepare, bcq_batch_prepare; 9: bcq_linear_fwd_lut;
+ * 10: bcq_logprobs_*, bcq_distill_*). */
 int bcq_abi_version(void);
 
 /* Scratch size (bytes) that enables the fastest path of `op` for this problem; *out may be 0.
@@ -355,6 +356,84 @@ bcq_status bcq_linear_bwd_alpha_adamw(const uint32_t* packed, const void* x, con
                                       int64_t N, int64_t K, int64_t g, int q, int q_train, float grad_scale,
                                       float* dalpha, float* alpha, float* m, float* v, const bcq_adamw* opt,
                                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Operators on logits: what a model answers and what it is adapted by -------------------------------------------
+ * logits x [T][V], fp32 or bf16, row t at x + t * row_stride elements (row_stride >= V: the columns of a padded vocabulary
+ * or a slice of a larger table); c = 1 / temperature.  With m = max_v x_v and S = sum_v exp((x_v - m) c),
+ *     ln q_v = (x_v - m) c - ln S        log probabilities of the row
+ * All sums, exponentials and logarithms are fp32 or wider; a gradient is rounded to `dtype` once.
+ *   - Limits: 0 <= T <= 2^24 (T = 0: nothing is done), 1 <= V <= BCQ_LOGITS_MAX_V, T * row_stride <= 2^40,
+ *     0 <= k <= BCQ_LOGITS_MAX_K, temperature finite and > 0 with a finite inverse; else BCQ_ERR_SHAPE.
+ *   - The pointers of these calls need the alignment of their elements only (a table of logits may start anywhere).
+ *   - Masked entries: -inf has probability 0 and no gradient; the lowest finite value is an ordinary value.  A row with
+ *     nothing left (-inf only): log probabilities -inf, lse -inf, entropy 0, gradient 0.  A row that holds a NaN or +inf:
+ *     its log probabilities, entropy, lse, loss and gradient are NaN.  Rows never influence each other.
+ *   - A gradient may be written over its logits (dlogits == logits and grad_stride == row_stride); other overlaps are not
+ *     allowed.
+ *   - No floating-point atomics: the results do not depend on the order in which workgroups run. */
+#define BCQ_LOGITS_MAX_V (1 << 20)
+#define BCQ_LOGITS_MAX_K 128
+
+typedef enum { BCQ_OP_LOGPROBS_FWD = 4, BCQ_OP_DISTILL_FWD = 5, BCQ_OP_DISTILL_FWD_BWD = 6 } bcq_logits_op;
+
+/* Device scratch of these calls (bytes; 0: none).  It is REQUIRED (BCQ_ERR_NULL without) where *out > 0.  Host-only. */
+bcq_status bcq_logits_workspace_bytes(int op, int64_t T, int64_t V, int k, int dtype, size_t* out);
+
+/* Log probabilities of given tokens, with the entropy and the k best alternatives of every row.  Every output may be NULL
+ * (it is then not computed); at least one is given.
+ *   tokens    [T] int64, in; NULL with logp NULL.  Negative: no token (logp 0); >= V: logp NaN
+ *   logp      [T] ln q of the token
+ *   entropy   [T] -sum_v q_v ln q_v
+ *   lse       [T] ln sum_v exp(x_v c) = m c + ln S
+ *   stats     [T][2] row statistics for bcq_logprobs_bwd
+ *   top_index [T][k] int32, top_logit [T][k] (x itself, as fp32), top_logp [T][k] (ln q): the k largest entries in falling
+ *             order, equal ones by rising index (-0 equals 0).  A NaN is no alternative; entries that are missing for
+ *             that (or for V < k) have index -1, top_logit -inf and top_logp NaN in a row that holds a NaN or +inf, else
+ *             -inf.  Read and written for k > 0 only.
+ * A row without a token is not read when nothing but logp and stats is asked for (its stats are then 0). */
+bcq_status bcq_logprobs_fwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride, const int64_t* tokens,
+                            float temperature, int k, float* logp, float* entropy, float* lse, float* stats,
+                            int32_t* top_index, float* top_logit, float* top_logp, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Gradient of sum_t dlogp[t] logp[t] + dentropy[t] entropy[t]:
+ *   dx_v = c (dlogp (1[v = token] - q_v) - dentropy q_v (ln q_v + entropy)).
+ *   tokens, dlogp [T] in (both NULL: no such term); entropy, dentropy [T] in (both NULL likewise), entropy as
+ *   bcq_logprobs_fwd returned it; stats as it returned them; dlogits [T][V] `dtype` out, rows of grad_stride.
+ * A row whose weights are both 0 (or that has no token and no entropy term) gets zeros and is not read. */
+bcq_status bcq_logprobs_bwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride, const int64_t* tokens,
+                            float temperature, const float* stats, const float* dlogp, const float* entropy,
+                            const float* dentropy, void* dlogits, int64_t grad_stride, void* stream);
+
+/* Distillation from a teacher's top logits.  The teacher's list of a row holds k (1 <= k <= BCQ_LOGITS_MAX_K) logits z_i and
+ * their indices j_i (j_i < 0: absent; >= V: the row's loss and gradient are NaN; an index that stands twice counts with
+ * both probabilities), ln p_i = z_i c - L:
+ *   teacher_lse NULL: L = ln sum_i exp(z_i c), the list is the whole distribution;
+ *   teacher_lse [T]:  L is the teacher's own ln sum_v exp(z_v c) over its vocabulary (the lse of bcq_logprobs_fwd at the same
+ *                     temperature), and r = max(0, 1 - sum_i p_i), the rest of its probability, is compared with the
+ *                     student's rest qbar = 1 - sum_{v in list} q_v as one outcome (both sums without cancellation).
+ *     loss[t] = (sum_i p_i (ln p_i - ln q_{j_i}) + r (ln r - ln qbar)) / c^2
+ * (the factor 1 / c^2 keeps the size of the gradient when the temperature changes).  p_i = 0 adds nothing; p_i > 0 where the
+ * student has probability 0 makes the loss +inf.  A row without a list has loss 0 and gradient 0.
+ *   top_logit, top_index [T][k] in; teacher_lse [T] in or NULL; loss [T] out; stats [T][4] out, for bcq_distill_bwd, or NULL. */
+bcq_status bcq_distill_fwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride, const float* top_logit,
+                           const int32_t* top_index, int k, const float* teacher_lse, float temperature, float* loss,
+                           float* stats, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradient of sum_t dloss[t] loss[t]; all inputs as given to and returned by bcq_distill_fwd.
+ *   listed:  dx_j = dloss (P q_j - p_j) / c    (P = sum_i p_i without teacher_lse, else 1)
+ *   others:  dx_v = dloss P q_v / c  without teacher_lse, else  dloss (q_v - r q_v / qbar) / c
+ * A row with dloss 0 gets zeros and is not read. */
+bcq_status bcq_distill_bwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride, const float* top_logit,
+                           const int32_t* top_index, int k, const float* teacher_lse, float temperature,
+                           const float* stats, const float* dloss, void* dlogits, int64_t grad_stride, void* stream);
+
+/* Both at once for a step that knows its rows' weights beforehand (1 / number of scored tokens, say): loss[t] as above and
+ * the gradient of sum_t weight[t] loss[t] (weight NULL: 1).  A row of weight 0 has loss 0 and is not read. */
+bcq_status bcq_distill_fwd_bwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride,
+                               const float* top_logit, const int32_t* top_index, int k, const float* teacher_lse,
+                               float temperature, const float* weight, float* loss, void* dlogits, int64_t grad_stride,
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -7,4 +7,6 @@ from .binding import (BatchPlan, BcqError, batch_plan, bcq_batch_prepare, bcq_li
                       bcq_linear_bwd_input, bcq_linear_bwd_input_grouped, bcq_linear_fwd, bcq_linear_fwd_decode,
                       bcq_linear_fwd_grouped, bcq_linear_fwd_lut, bcq_linear_fwd_static, bcq_pack_decode, decode_layout_bytes,
                       bcq_pack, bcq_pack_transposed, bcq_quantize, bcq_quantize_alternating, bcq_quantize_grouped, bcq_unpack, load,
-                      status_string, workspace_bytes, workspace_bytes_grouped)
+                      status_string, workspace_bytes, workspace_bytes_grouped,
+                      Logprobs, bcq_distill_bwd, bcq_distill_fwd, bcq_distill_fwd_bwd, bcq_logprobs_bwd, bcq_logprobs_fwd,
+                      logits_workspace_bytes)

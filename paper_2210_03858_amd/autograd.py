@@ -3,9 +3,11 @@ scales are trained; Section 4.2: normally alpha_1 alone).
 
 `BCQLinearFunction` routes forward (Eq. 2), input gradient (Eq. 3) and scale gradient (Eq. 4) to the C-ABI entry
 points; `BCQLinear` is the module around it, which takes the same node in native code (csrc/bcq_torch.cpp) for plain
-tensors outside of transforms and traces.  Nothing is computed here: every product runs in the HIP kernels.
+tensors outside of transforms and traces.  `token_logprobs` and `distill_loss` are the differentiable forms of the
+operators on logits.  Nothing is computed here: every product runs in the HIP kernels.
 """
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -98,3 +100,74 @@ class BCQLinear(torch.nn.Module):
         if y is None:
             y = BCQLinearFunction.apply(x, self.alpha_train, self.alpha_frozen, layer)
         return y if self.bias is None else y + self.bias.to(y.dtype)
+
+
+class TokenLogprobsFunction(torch.autograd.Function):
+    """(logp, entropy or an empty tensor) of logits [T, V]; the gradient reads the logits again."""
+
+    @staticmethod
+    def forward(ctx, logits, tokens, temperature, want_entropy):
+        out = B.bcq_logprobs_fwd(logits, tokens, temperature=temperature, entropy=want_entropy, stats=True)
+        ctx.temperature = temperature
+        ctx.save_for_backward(logits, tokens, out.stats, out.entropy)
+        ctx.set_materialize_grads(False)
+        return out.logp, out.entropy
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dlogp, dentropy):
+        logits, tokens, stats, entropy = ctx.saved_tensors
+        if dlogp is None and dentropy is None:
+            return None, None, None, None
+        dx = B.bcq_logprobs_bwd(logits, stats, tokens if dlogp is not None else None,
+                                None if dlogp is None else dlogp.contiguous(),
+                                None if dentropy is None else entropy, None if dentropy is None else dentropy.contiguous(),
+                                temperature=ctx.temperature)
+        return dx, None, None, None
+
+
+class DistillLossFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, top_logit, top_index, teacher_lse, temperature):
+        stats = torch.empty((logits.shape[0], 4), dtype=torch.float32, device=logits.device)
+        loss = B.bcq_distill_fwd(logits, top_logit, top_index, teacher_lse, temperature=temperature, stats=stats)
+        ctx.temperature = temperature
+        ctx.save_for_backward(logits, top_logit, top_index, teacher_lse, stats)
+        return loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        logits, top_logit, top_index, teacher_lse, stats = ctx.saved_tensors
+        dx = B.bcq_distill_bwd(logits, top_logit, top_index, stats, dloss.contiguous(), teacher_lse,
+                               temperature=ctx.temperature)
+        return dx, None, None, None, None
+
+
+def _flat(t, tail):
+    """t [..., tail] as rows; None stays None."""
+    return None if t is None else t.reshape(-1, *tail).contiguous()
+
+
+def _rows(logits):
+    """logits [..., V] as a table whose rows are contiguous, copied only where they are not."""
+    rows = logits.reshape(-1, logits.shape[-1])
+    return rows if rows.stride(1) == 1 else rows.contiguous()
+
+
+def token_logprobs(logits, tokens, temperature=1.0, entropy=False):
+    """ln softmax(logits / temperature) at tokens, and the entropy of every row (None unless asked for), differentiable
+    with respect to the logits.  logits [..., V] fp32 or bf16; tokens [...] int64, negative where there is none (0, no
+    gradient)."""
+    shape = logits.shape[:-1]
+    logp, H = TokenLogprobsFunction.apply(_rows(logits), _flat(tokens, ()), float(temperature), bool(entropy))
+    return logp.reshape(shape), None if H is None else H.reshape(shape)
+
+
+def distill_loss(logits, top_logit, top_index, teacher_lse=None, temperature=1.0):
+    """Loss [...] of logits [..., V] against a teacher's list (top_logit fp32 and top_index int32 [..., k]), with
+    teacher_lse [...] also against the rest of its vocabulary; differentiable with respect to the logits."""
+    shape, k = logits.shape[:-1], top_index.shape[-1]
+    loss = DistillLossFunction.apply(_rows(logits), _flat(top_logit, (k,)), _flat(top_index, (k,)),
+                                     _flat(teacher_lse, ()), float(temperature))
+    return loss.reshape(shape)

@@ -6,6 +6,7 @@ only), checks dtype/shape/contiguity on the host, passes raw device pointers and
 the C entry point of the same name, and raises BcqError on a non-zero status.  There is no CPU fallback:
 if the shared library is missing, load() raises.
 """
+import collections
 import ctypes
 import os
 import warnings
@@ -17,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libbcq_hip.so")
 
 BCQ_F32, BCQ_BF16 = 0, 1
 OP_QUANTIZE, OP_FWD, OP_BWD_INPUT, OP_BWD_ALPHA = 0, 1, 2, 3
+OP_LOGPROBS_FWD, OP_DISTILL_FWD, OP_DISTILL_FWD_BWD = 4, 5, 6
 QUANTIZE_MAX_K = 16384
 
 EXPORTS = ("bcq_status_string", "bcq_abi_version", "bcq_workspace_bytes", "bcq_quantize", "bcq_pack",
@@ -25,7 +27,8 @@ EXPORTS = ("bcq_status_string", "bcq_abi_version", "bcq_workspace_bytes", "bcq_q
            "bcq_linear_bwd_input_grouped", "bcq_linear_bwd_alpha_grouped", "bcq_quantize_alternating",
            "bcq_alpha_adamw_step", "bcq_linear_bwd_alpha_adamw", "bcq_decode_layout_bytes", "bcq_pack_decode",
            "bcq_linear_fwd_decode", "bcq_linear_fwd_static", "bcq_linear_fwd_lut", "bcq_batch_sizes", "bcq_batch_plan", "bcq_linear_batched",
-           "bcq_prepare", "bcq_batch_prepare")
+           "bcq_prepare", "bcq_batch_prepare", "bcq_logits_workspace_bytes", "bcq_logprobs_fwd", "bcq_logprobs_bwd",
+           "bcq_distill_fwd", "bcq_distill_bwd", "bcq_distill_fwd_bwd")
 
 _lib = None
 _native = None  # False: not there
@@ -92,6 +95,12 @@ def load():
     lib.bcq_linear_batched.argtypes = [vp, vp, sz, vp, sz, vp]
     lib.bcq_prepare.argtypes = [i32, i64, i64, i64, i64, i32, i32]
     lib.bcq_batch_prepare.argtypes = [vp, sz]
+    lib.bcq_logits_workspace_bytes.argtypes = [i32, i64, i64, i32, i32, ctypes.POINTER(sz)]
+    lib.bcq_logprobs_fwd.argtypes = [vp, i32, i64, i64, i64, vp, f32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bcq_logprobs_bwd.argtypes = [vp, i32, i64, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    lib.bcq_distill_fwd.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, vp, f32, vp, vp, vp, sz, vp]
+    lib.bcq_distill_bwd.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, vp, f32, vp, vp, vp, i64, vp]
+    lib.bcq_distill_fwd_bwd.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, vp, f32, vp, vp, vp, i64, vp, sz, vp]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = i32
     _lib = lib
@@ -593,3 +602,159 @@ def bcq_batch_prepare(plan):
 def bcq_prepare(op, T, N, K, q, dtype=BCQ_BF16, g=None):
     """Host-side set-up for later calls of `op` with these shapes (before a first call inside a graph capture)."""
     _check(load().bcq_prepare(op, T, N, K, K if g is None else int(g), q, dtype), "bcq_prepare")
+
+
+# ---- operators on logits [T, V]: log probabilities, entropy, best alternatives; distillation from a teacher's list --------
+
+LOGITS_MAX_V, LOGITS_MAX_K = 1 << 20, 128
+
+Logprobs = collections.namedtuple("Logprobs", "logp entropy lse stats top_index top_logit top_logp", defaults=(None,) * 7)
+
+
+def logits_workspace_bytes(op, T, V, k, dtype):
+    out = ctypes.c_size_t(0)
+    _check(load().bcq_logits_workspace_bytes(op, T, V, k, dtype, ctypes.byref(out)), "bcq_logits_workspace_bytes")
+    return int(out.value)
+
+
+def _table(t, name, like=None):
+    """(T, V, row stride) of a table of logits: rows of contiguous entries, any distance from row to row."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and (like is None or (t.dtype == like.dtype
+            and t.shape == like.shape))):
+        raise ValueError("%s must be a 2-dimensional cuda tensor%s" % (name, "" if like is None else " like logits"))
+    T, V = t.shape
+    stride = t.stride(0) if T > 1 else max(V, 1)
+    if (V > 1 and t.stride(1) != 1) or stride < V:
+        raise ValueError("the rows of %s must be contiguous and must not overlap" % name)
+    return T, V, stride
+
+
+def _logits_scratch(op, T, V, k, dt, like, workspace):
+    """The caller's workspace, or one from torch's caching allocator (it belongs to the stream of the call)."""
+    if workspace is None:
+        n = logits_workspace_bytes(op, T, V, k, dt)
+        workspace = torch.empty((n,), dtype=torch.uint8, device=like.device) if n else None
+    return workspace
+
+
+def bcq_logprobs_fwd(logits, tokens=None, k=0, temperature=1.0, entropy=False, lse=False, stats=False, out=None,
+                     workspace=None):
+    """Log probabilities of one token per row, with what else is asked for -> Logprobs (None where not asked for).
+
+    logits [T, V] fp32 or bf16 (rows may lie apart); tokens [T] int64, negative for none.  k > 0: the k best entries
+    (top_index int32, top_logit, top_logp, each [T, k]).  stats: what bcq_logprobs_bwd needs.  out: a Logprobs with the
+    tensors to fill instead; its fields say what is computed."""
+    T, V, stride = _table(logits, "logits")
+    dt = _act_dtype(logits)
+    k = int(k)
+    if tokens is not None:
+        _need(tokens, torch.int64, (T,), "tokens")
+    if out is None:
+        def new(wanted, shape, dtype=torch.float32):
+            return torch.empty(shape, dtype=dtype, device=logits.device) if wanted else None
+        top = (T, max(k, 0))
+        out = Logprobs(new(tokens is not None, (T,)), new(entropy, (T,)), new(lse, (T,)), new(stats, (T, 2)),
+                       new(k > 0, top, torch.int32), new(k > 0, top), new(k > 0, top))
+    else:
+        shapes = ((T,), (T,), (T,), (T, 2), (T, k), (T, k), (T, k))
+        for name, t, shape in zip(Logprobs._fields, out, shapes):
+            if t is not None:
+                _need(t, torch.int32 if name == "top_index" else torch.float32, shape, name)
+    if T == 0:
+        return out
+    workspace = _logits_scratch(OP_LOGPROBS_FWD, T, V, k, dt, logits, workspace)
+    wp, wb = _ws(workspace)
+    _check(load().bcq_logprobs_fwd(_ptr(logits), dt, T, V, stride, _ptr(tokens), float(temperature), k, *map(_ptr, out),
+                                   wp, wb, _stream()), "bcq_logprobs_fwd")
+    return out
+
+
+def bcq_logprobs_bwd(logits, stats, tokens=None, dlogp=None, entropy=None, dentropy=None, temperature=1.0, dlogits=None):
+    """Gradient of sum(dlogp * logp) + sum(dentropy * entropy) with respect to the logits; dlogits may be logits itself."""
+    T, V, stride = _table(logits, "logits")
+    dt = _act_dtype(logits)
+    _need(stats, torch.float32, (T, 2), "stats")
+    if tokens is not None:
+        _need(tokens, torch.int64, (T,), "tokens")
+    for t, name in ((dlogp, "dlogp"), (entropy, "entropy"), (dentropy, "dentropy")):
+        if t is not None:
+            _need(t, torch.float32, (T,), name)
+    dlogits = torch.empty((T, V), dtype=logits.dtype, device=logits.device) if dlogits is None else dlogits
+    _, _, gstride = _table(dlogits, "dlogits", logits)
+    if T == 0:
+        return dlogits
+    _check(load().bcq_logprobs_bwd(_ptr(logits), dt, T, V, stride, _ptr(tokens), float(temperature), _ptr(stats),
+                                   _ptr(dlogp), _ptr(entropy), _ptr(dentropy), _ptr(dlogits), gstride, _stream()),
+           "bcq_logprobs_bwd")
+    return dlogits
+
+
+def _list(top_logit, top_index, teacher_lse, T):
+    if not (isinstance(top_index, torch.Tensor) and top_index.dim() == 2):
+        raise ValueError("top_index must be a 2-dimensional tensor")
+    k = top_index.shape[1]
+    _need(top_index, torch.int32, (T, k), "top_index")
+    _need(top_logit, torch.float32, (T, k), "top_logit")
+    if teacher_lse is not None:
+        _need(teacher_lse, torch.float32, (T,), "teacher_lse")
+    return k
+
+
+def bcq_distill_fwd(logits, top_logit, top_index, teacher_lse=None, temperature=1.0, loss=None, stats=None, workspace=None):
+    """Distillation loss [T] against a teacher's list (top_logit [T, k] fp32, top_index [T, k] int32, negative for none);
+    teacher_lse [T]: the rest of the teacher's vocabulary counts as one outcome.  stats [T, 4], when given, is filled for
+    bcq_distill_bwd."""
+    T, V, stride = _table(logits, "logits")
+    dt = _act_dtype(logits)
+    k = _list(top_logit, top_index, teacher_lse, T)
+    loss = torch.empty((T,), dtype=torch.float32, device=logits.device) if loss is None else loss
+    _need(loss, torch.float32, (T,), "loss")
+    if stats is not None:
+        _need(stats, torch.float32, (T, 4), "stats")
+    if T == 0:
+        return loss
+    workspace = _logits_scratch(OP_DISTILL_FWD, T, V, k, dt, logits, workspace)
+    wp, wb = _ws(workspace)
+    _check(load().bcq_distill_fwd(_ptr(logits), dt, T, V, stride, _ptr(top_logit), _ptr(top_index), k, _ptr(teacher_lse),
+                                  float(temperature), _ptr(loss), _ptr(stats), wp, wb, _stream()), "bcq_distill_fwd")
+    return loss
+
+
+def bcq_distill_bwd(logits, top_logit, top_index, stats, dloss, teacher_lse=None, temperature=1.0, dlogits=None):
+    """Gradient of sum(dloss * loss) with respect to the logits; dlogits may be logits itself."""
+    T, V, stride = _table(logits, "logits")
+    dt = _act_dtype(logits)
+    k = _list(top_logit, top_index, teacher_lse, T)
+    _need(stats, torch.float32, (T, 4), "stats")
+    _need(dloss, torch.float32, (T,), "dloss")
+    dlogits = torch.empty((T, V), dtype=logits.dtype, device=logits.device) if dlogits is None else dlogits
+    _, _, gstride = _table(dlogits, "dlogits", logits)
+    if T == 0:
+        return dlogits
+    _check(load().bcq_distill_bwd(_ptr(logits), dt, T, V, stride, _ptr(top_logit), _ptr(top_index), k, _ptr(teacher_lse),
+                                  float(temperature), _ptr(stats), _ptr(dloss), _ptr(dlogits), gstride, _stream()),
+           "bcq_distill_bwd")
+    return dlogits
+
+
+def bcq_distill_fwd_bwd(logits, top_logit, top_index, weight=None, teacher_lse=None, temperature=1.0, loss=None, dlogits=None,
+                        workspace=None):
+    """Loss [T] and the gradient of sum(weight * loss) in one call -> (loss, dlogits); rows of weight 0 are skipped.
+    dlogits may be logits itself."""
+    T, V, stride = _table(logits, "logits")
+    dt = _act_dtype(logits)
+    k = _list(top_logit, top_index, teacher_lse, T)
+    if weight is not None:
+        _need(weight, torch.float32, (T,), "weight")
+    loss = torch.empty((T,), dtype=torch.float32, device=logits.device) if loss is None else loss
+    _need(loss, torch.float32, (T,), "loss")
+    dlogits = torch.empty((T, V), dtype=logits.dtype, device=logits.device) if dlogits is None else dlogits
+    _, _, gstride = _table(dlogits, "dlogits", logits)
+    if T == 0:
+        return loss, dlogits
+    workspace = _logits_scratch(OP_DISTILL_FWD_BWD, T, V, k, dt, logits, workspace)
+    wp, wb = _ws(workspace)
+    _check(load().bcq_distill_fwd_bwd(_ptr(logits), dt, T, V, stride, _ptr(top_logit), _ptr(top_index), k,
+                                      _ptr(teacher_lse), float(temperature), _ptr(weight), _ptr(loss), _ptr(dlogits),
+                                      gstride, wp, wb, _stream()), "bcq_distill_fwd_bwd")
+    return loss, dlogits

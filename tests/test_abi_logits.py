@@ -1,0 +1,130 @@
+"""Host-side checks of the entry points on logits (no GPU needed): every argument error is reported before any device is
+touched, in the order NULL, shape, dtype, alignment, workspace, device."""
+import ctypes
+import os
+
+import pytest
+
+A = 0x1000  # a fake, aligned, never dereferenced pointer
+I64 = ctypes.c_int64
+NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, DEVICE = 1, 2, 3, 4, 5, 7
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2210_03858_amd import binding, build
+    if not os.path.exists(binding.LIB_PATH):
+        build.build_library()
+    return binding.load()
+
+
+def logprobs(lib, x=A, dtype=1, T=4, V=100, stride=100, tokens=A, tau=1.0, k=5, logp=A, entropy=A, lse=A, stats=A, index=A,
+             logit=A, top=A, ws=None, ws_bytes=0):
+    return lib.bcq_logprobs_fwd(x, dtype, I64(T), I64(V), I64(stride), tokens, tau, k, logp, entropy, lse, stats, index, logit,
+                                top, ws, ws_bytes, None)
+
+
+def logprobs_bwd(lib, x=A, dtype=1, T=4, V=100, stride=100, tokens=A, tau=1.0, stats=A, dlogp=A, entropy=A, dentropy=A,
+                 dx=A + 4096, dstride=100):
+    return lib.bcq_logprobs_bwd(x, dtype, I64(T), I64(V), I64(stride), tokens, tau, stats, dlogp, entropy, dentropy, dx,
+                                I64(dstride), None)
+
+
+def distill(lib, x=A, dtype=1, T=4, V=100, stride=100, logit=A, index=A, k=5, lse=A, tau=1.0, loss=A, stats=A, ws=A,
+            ws_bytes=1 << 30):
+    return lib.bcq_distill_fwd(x, dtype, I64(T), I64(V), I64(stride), logit, index, k, lse, tau, loss, stats, ws, ws_bytes, None)
+
+
+def distill_bwd(lib, x=A, dtype=1, T=4, V=100, stride=100, logit=A, index=A, k=5, lse=A, tau=1.0, stats=A, dloss=A,
+                dx=A + 4096, dstride=100):
+    return lib.bcq_distill_bwd(x, dtype, I64(T), I64(V), I64(stride), logit, index, k, lse, tau, stats, dloss, dx, I64(dstride),
+                               None)
+
+
+def distill_both(lib, x=A, dtype=1, T=4, V=100, stride=100, logit=A, index=A, k=5, lse=A, tau=1.0, weight=A, loss=A,
+                 dx=A + 4096, dstride=100, ws=A, ws_bytes=1 << 30):
+    return lib.bcq_distill_fwd_bwd(x, dtype, I64(T), I64(V), I64(stride), logit, index, k, lse, tau, weight, loss, dx,
+                                   I64(dstride), ws, ws_bytes, None)
+
+
+CALLS = [logprobs, logprobs_bwd, distill, distill_bwd, distill_both]
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_shapes(lib, call):
+    assert call(lib, T=-1) == SHAPE
+    assert call(lib, T=(1 << 24) + 1) == SHAPE
+    assert call(lib, V=0) == SHAPE
+    assert call(lib, V=(1 << 20) + 1, stride=1 << 21) == SHAPE
+    assert call(lib, stride=99) == SHAPE
+    assert call(lib, T=1 << 24, stride=1 << 17) == SHAPE          # more than 2^40 entries
+    assert call(lib, stride=(1 << 63) - 1) == SHAPE
+    for tau in (0.0, -1.0, float("inf"), float("nan"), 1e-45):
+        assert call(lib, tau=tau) == SHAPE, tau
+    if call is not logprobs_bwd:
+        assert call(lib, k=-1) == SHAPE
+        assert call(lib, k=129) == SHAPE
+    if call not in (logprobs, logprobs_bwd):
+        assert call(lib, k=0) == SHAPE
+    if "dstride" in call.__code__.co_varnames:
+        assert call(lib, dstride=99) == SHAPE
+        assert call(lib, dx=A, dstride=128) == SHAPE              # over its own logits with rows elsewhere
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_dtype_and_alignment(lib, call):
+    assert call(lib, dtype=2) == DTYPE
+    assert call(lib, dtype=-1) == DTYPE
+    assert call(lib, x=A + 1) == ALIGN
+    assert call(lib, x=A + 2, dtype=0) == ALIGN
+    for name in ("tokens", "logp", "entropy", "lse", "stats", "index", "logit", "top", "dlogp", "dentropy", "dx", "loss",
+                 "dloss", "weight"):
+        if name in call.__code__.co_varnames:
+            assert call(lib, **{name: A + 1}) == ALIGN, name
+    if "tokens" in call.__code__.co_varnames:
+        assert call(lib, tokens=A + 4) == ALIGN
+
+
+def test_null(lib):
+    assert logprobs(lib, x=None) == NULL
+    assert logprobs(lib, tokens=None) == NULL and logprobs(lib, logp=None) == NULL
+    none = dict(tokens=None, logp=None, entropy=None, lse=None, stats=None)
+    assert logprobs(lib, index=None, logit=None, top=None, **none) == NULL     # nothing asked for
+    assert logprobs(lib, k=0, **none) == NULL
+    for name in ("x", "stats", "dx", "tokens", "dlogp", "entropy", "dentropy"):
+        assert logprobs_bwd(lib, **{name: None}) == NULL, name
+    assert logprobs_bwd(lib, tokens=None, dlogp=None, entropy=None, dentropy=None) == NULL
+    for call in (distill, distill_bwd, distill_both):
+        for name in ("x", "logit", "index", "loss", "stats", "dloss", "dx"):
+            if name in call.__code__.co_varnames and not (call is distill and name == "stats"):
+                assert call(lib, **{name: None}) == NULL, (call, name)
+
+
+def test_workspace(lib):
+    out = ctypes.c_size_t(77)
+    size = lib.bcq_logits_workspace_bytes
+    assert size(4, I64(8), I64(1000), 5, 1, None) == NULL
+    assert size(3, I64(8), I64(1000), 5, 1, ctypes.byref(out)) == DTYPE and size(7, I64(8), I64(1000), 5, 1, ctypes.byref(out)) == DTYPE
+    assert size(4, I64(8), I64(1000), 5, 2, ctypes.byref(out)) == DTYPE
+    assert size(4, I64(8), I64(1000), 129, 1, ctypes.byref(out)) == SHAPE
+    assert size(5, I64(8), I64(1000), 0, 1, ctypes.byref(out)) == SHAPE
+    assert size(6, I64(-1), I64(1000), 5, 1, ctypes.byref(out)) == SHAPE
+    assert out.value == 77
+    for op, call in ((4, logprobs), (5, distill), (6, distill_both)):
+        for T, V, dtype in ((1, 50257, 1), (64, 50257, 0), (3, 1 << 20, 0), (4096, 50257, 1), (0, 8, 1)):
+            assert size(op, I64(T), I64(V), 5, dtype, ctypes.byref(out)) == 0
+            if out.value:
+                args = dict(T=T, V=V, stride=V, dtype=dtype)
+                if call is distill_both:
+                    args["dstride"] = V
+                assert call(lib, ws=None, ws_bytes=0, **args) == NULL
+                assert call(lib, ws=A, ws_bytes=out.value - 1, **args) == WORKSPACE
+                assert call(lib, ws=A + 8, ws_bytes=out.value, **args) == ALIGN
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_no_device_comes_last(lib, call):
+    import torch
+    if not torch.cuda.is_available():
+        extra = dict(ws=A, ws_bytes=1 << 30) if "ws" in call.__code__.co_varnames else {}
+        assert call(lib, **extra) == DEVICE

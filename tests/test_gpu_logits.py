@@ -1,0 +1,511 @@
+"""Operators on logits against their definition in 64 bits (plain torch operations).
+
+Tolerances, from the arithmetic (d = (x - m) c, three roundings of 2^-24 each on d log2(e) and one on the exponential):
+  values     the entries that carry a row's sums lie within 16 or so of its maximum: 3 * 16 * 2^-24 < 2^-18 of 1 + |value|
+  gradients  an entry's probability is off by at most |d| 2^-22 of itself, |d| < 128: 2^-15 of the entry's terms, and half a
+             unit in the last place of bf16 (2^-9) where that is the type; below 2^-100 everything counts as 0
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2210_03858_amd as bcq
+from paper_2210_03858_amd import autograd
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+VALUE, GRAD = 2.0 ** -18, 2.0 ** -15
+
+
+def table(T, V, dtype, seed=0, stride=None, offset=0, scale=2.5):
+    """Logits [T, V] on the GPU, rows `stride` apart, the first `offset` elements into the allocation."""
+    stride = V if stride is None else stride
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn((T, V), generator=gen) * scale
+    x[:, torch.randint(V, (max(1, V // 5000),), generator=gen)] += 9.0
+    buf = torch.zeros((T * stride + offset,), dtype=DTYPES[dtype], device="cuda")
+    t = buf[offset:].as_strided((T, V), (stride, 1), buf.storage_offset() + offset)
+    t.copy_(x)
+    return t
+
+
+def tokens_for(T, V, seed=0):
+    tok = torch.randint(V, (T,), generator=torch.Generator().manual_seed(seed + 1))
+    tok[::5] = -100 if T > 1 else tok[0]
+    return tok
+
+
+def reference(x, tok, tau):
+    """ln q [T, V], logp, entropy, lse in 64 bits."""
+    y = x.detach().double() / tau
+    tok = None if tok is None else tok.to(y.device)
+    top = y.max(1, keepdim=True).values
+    top = torch.where(torch.isneginf(top), 0.0, top)
+    s = torch.exp(y - top).sum(1, keepdim=True)
+    logq = torch.where(s == 0, -INF, y - top - torch.log(s))
+    q = torch.exp(logq)
+    H = -torch.where(q == 0, 0.0, q * logq).sum(1)
+    lse = (top + torch.log(s))[:, 0]
+    logp = torch.where(tok < 0, 0.0, logq.gather(1, tok.clamp(min=0)[:, None])[:, 0]) if tok is not None else None
+    return logq, logp, H, lse
+
+
+def best(x, k):
+    """Indices of the k largest, the lowest index first among equals; -1 where there are not as many."""
+    T, V = x.shape
+    out = torch.full((T, k), -1, dtype=torch.int32)
+    row = x.double().cpu() + 0.0 if T * V < 1 << 20 else x.double() + 0.0
+    # NaN last: behind the -inf, whose order among themselves the stable sort keeps
+    order = torch.sort(torch.where(torch.isnan(row), -INF, row), dim=1, descending=True, stable=True).indices
+    nan = torch.isnan(row).gather(1, order)
+    if nan.any():
+        order = order.gather(1, torch.sort(nan.int(), dim=1, stable=True).indices)
+    n = (~torch.isnan(row)).sum(1, keepdim=True).cpu()
+    first = order[:, :k].int().cpu()
+    out[:, :first.shape[1]] = torch.where(torch.arange(first.shape[1]) < n, first, -1)
+    return out
+
+
+def close(got, ref, scale=None):
+    ref = ref.double()
+    got = got.detach().double().to(ref.device)
+    assert torch.equal(torch.isfinite(got), torch.isfinite(ref))
+    assert torch.equal(got[torch.isinf(ref)], ref[torch.isinf(ref)]) and torch.equal(torch.isnan(got), torch.isnan(ref))
+    ok = torch.isfinite(ref)
+    bound = VALUE * (1.0 + ref.abs() if scale is None else scale)
+    bad = ok & ~((got - ref).abs() <= bound)
+    assert not bad.any(), (got[bad][:4], ref[bad][:4])
+
+
+def close_grad(got, ref, terms):
+    """|got - ref| within GRAD of the terms' magnitudes, and bf16's rounding."""
+    rounding = 2.0 ** -8 if got.dtype == torch.bfloat16 else 2.0 ** -23
+    got, ref = got.double().to(ref.device), ref.double()
+    assert torch.equal(torch.isnan(got), torch.isnan(ref))
+    bad = ~torch.isnan(ref) & ~((got - ref).abs() <= GRAD * terms + rounding * ref.abs() + 2.0 ** -100)
+    assert not bad.any(), (got[bad][:4], ref[bad][:4], bad.nonzero()[:4])
+
+
+SHAPES = [  # T, V, stride, offset
+    (1, 1, None, 0), (3, 2, None, 0), (1, 7, None, 0), (2, 8, None, 0), (5, 31, 33, 1), (3, 130, None, 3), (300, 257, None, 0),
+    (4, 1000, 1003, 5), (7, 4099, None, 0), (2, 32003, 32064, 0), (1, 50257, None, 0), (6, 50257, None, 7),
+    (1100, 5003, None, 0), (520, 33001, None, 1), (2, 65537, None, 0), (3, 131075, 131077, 0), (1, 250007, None, 0), (300, 140001, None, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,stride,offset", SHAPES)
+def test_logprobs_values(T, V, stride, offset, dtype):
+    x = table(T, V, dtype, seed=V, stride=stride, offset=offset)
+    tok, tau = tokens_for(T, V), 0.7 if V % 2 else 1.0
+    k = min(V, (20, 5, 128)[V % 3])
+    out = bcq.bcq_logprobs_fwd(x, tok.cuda(), k=k, temperature=tau, entropy=True, lse=True, stats=True)
+    logq, logp, H, lse = reference(x, tok, tau)
+    close(out.logp, logp)
+    close(out.entropy, H, 1.0 + math.log(V) + H)
+    close(out.lse, lse)
+    index = best(x, k)
+    assert torch.equal(out.top_index.cpu(), index)
+    assert torch.equal(out.top_logit.cpu(), x.float().cpu().gather(1, index.long()))
+    close(out.top_logp, logq.gather(1, index.long().cuda()))
+    # asked for alone, every output is the same
+    alone = bcq.bcq_logprobs_fwd(x, tok.cuda(), temperature=tau)
+    assert alone.entropy is None and alone.top_index is None
+    close(alone.logp, logp)
+    top = bcq.bcq_logprobs_fwd(x, k=k, temperature=tau)
+    assert top.logp is None and torch.equal(top.top_index.cpu(), index)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,stride,offset", SHAPES)
+def test_logprobs_gradient(T, V, stride, offset, dtype):
+    x = table(T, V, dtype, seed=V + 1, stride=stride, offset=offset)
+    tok, tau = tokens_for(T, V, 3), 1.0 if V % 2 else 0.8
+    gen = torch.Generator().manual_seed(5)
+    g, h = torch.randn((T,), generator=gen), 0.1 * torch.randn((T,), generator=gen)
+    if T > 3:
+        h[3] = 0.0
+    logq, _, H, _ = reference(x, tok, tau)
+    q = torch.exp(logq)
+    tok, g, h = tok.cuda(), g.cuda(), h.cuda()
+    given = (tok >= 0).double()[:, None]
+    unit = torch.zeros_like(q).scatter_(1, tok.clamp(min=0)[:, None], 1.0)
+    first = given * g.double()[:, None] * (unit - q) / tau
+    second = -h.double()[:, None] * torch.where(q == 0, 0.0, q * (logq + H[:, None])) / tau
+    size1 = given * g.double().abs()[:, None] * (unit + q) / tau
+    size2 = h.double().abs()[:, None] * torch.where(q == 0, 0.0, q * (logq.abs() + H[:, None])) / tau
+    out = bcq.bcq_logprobs_fwd(x, tok, temperature=tau, entropy=True, stats=True)
+    both = bcq.bcq_logprobs_bwd(x, out.stats, tok, g, out.entropy, h, temperature=tau)
+    close_grad(both, first + second, size1 + size2)
+    close_grad(bcq.bcq_logprobs_bwd(x, out.stats, tok, g, temperature=tau), first, size1)
+    close_grad(bcq.bcq_logprobs_bwd(x, out.stats, None, None, out.entropy, h, temperature=tau), second, size2)
+    # over the logits themselves, and into rows of another distance and alignment
+    wide = torch.full((T, V + 3), 7.0, dtype=x.dtype, device="cuda")
+    bcq.bcq_logprobs_bwd(x, out.stats, tok, g, out.entropy, h, temperature=tau, dlogits=wide[:, 1:V + 1])
+    assert torch.equal(wide[:, 1:V + 1], both) and (wide[:, 0] == 7).all() and (wide[:, V + 1:] == 7).all()
+    bcq.bcq_logprobs_bwd(x, out.stats, tok, g, out.entropy, h, temperature=tau, dlogits=x)
+    assert torch.equal(x, both)
+
+
+def teacher(x, k, tau, seed=0):
+    gen = torch.Generator().manual_seed(seed)
+    z = 0.8 * x.float() + torch.randn(x.shape, generator=gen).cuda()
+    b = z.topk(k, dim=1)
+    return b.values.cpu(), b.indices.int().cpu(), torch.logsumexp(z.double() / tau, 1).float().cpu()
+
+
+def distill_reference(x, z, j, lse, tau):
+    """loss [T], gradient [T, V] of its sum and the magnitude of both's terms, in 64 bits; j < 0 is absent."""
+    logq, *_ = reference(x, None, tau)
+    q = torch.exp(logq)
+    z, j, lse = z.cuda(), j.cuda(), None if lse is None else lse.cuda()
+    here = j >= 0
+    jl = j.long().clamp(min=0)
+    lz = torch.where(here, z.double() / tau, -INF)
+    alone = torch.logsumexp(lz, 1)
+    L = torch.where(torch.isneginf(alone), 0.0, alone) if lse is None else lse.double()
+    lp = lz - L[:, None]
+    p = torch.exp(lp)
+    lq = logq.gather(1, jl)
+    loss = torch.where(p == 0, 0.0, p * (lp - lq)).sum(1)
+    size = torch.where(p == 0, 0.0, p * (lp.abs() + lq.abs())).sum(1)
+    target = torch.zeros_like(q).scatter_add_(1, jl, p)
+    inside = torch.zeros_like(q).scatter_add_(1, jl, here.double()) > 0
+    total = p.sum(1, keepdim=True)
+    if lse is not None:
+        r = (1.0 - total[:, 0]).clamp(min=0.0)
+        r = torch.where(inside.all(1), 0.0, r)
+        lrest = torch.logsumexp(torch.where(inside, -INF, logq), 1)
+        loss = loss + torch.where(r == 0, 0.0, r * (torch.log(r) - lrest))
+        size = size + torch.where(r == 0, 0.0, r * (torch.log(r).abs() + lrest.abs()))
+        target = target + torch.where(inside | (logq == -INF), 0.0, r[:, None] * torch.exp(logq - lrest[:, None]))
+        total = torch.ones_like(total)
+    empty = ~here.any(1)
+    nothing = torch.isneginf(logq).all(1)
+    grad = torch.where((empty | nothing)[:, None], 0.0, (total * q - target) * tau)
+    return torch.where(empty, 0.0, loss * tau * tau), grad, (total * q + target) * tau, (1.0 + size) * tau * tau
+
+
+def run_distill(x, z, j, lse, tau, weight):
+    """Loss and gradient in two calls, and both in one."""
+    z, j, lse = z.cuda(), j.cuda(), None if lse is None else lse.cuda()
+    T = x.shape[0]
+    stats = torch.empty((T, 4), device="cuda")
+    loss = bcq.bcq_distill_fwd(x, z, j, lse, temperature=tau, stats=stats)
+    grad = bcq.bcq_distill_bwd(x, z, j, stats, weight.cuda(), lse, temperature=tau)
+    return loss, grad, bcq.bcq_distill_fwd_bwd(x, z, j, weight=weight.cuda(), teacher_lse=lse, temperature=tau)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,stride,offset", SHAPES)
+def test_distill(T, V, stride, offset, dtype, rest):
+    x = table(T, V, dtype, seed=V + 2, stride=stride, offset=offset)
+    tau, k = (2.0, 1.0, 0.5)[V % 3], min(V, (64, 7, 128)[V % 3])
+    z, j, lse = teacher(x, k, tau)
+    j = j.clone()
+    if T > 2 and k > 2:
+        j[1, k // 2] = -1       # a shorter list
+        j[2] = -1               # no list
+    lse = lse if rest else None
+    w = torch.rand((T,), generator=torch.Generator().manual_seed(9)) + 0.5
+    if T > 4:
+        w[4] = 0.0
+    ref_loss, ref_grad, terms, size = distill_reference(x, z, j, lse, tau)
+    loss, grad, (loss2, grad2) = run_distill(x, z, j, lse, tau, w)
+    close(loss, ref_loss, size)
+    wd = w.double().cuda()[:, None]
+    close_grad(grad, ref_grad * wd, terms * wd)
+    close(loss2, torch.where(w.cuda() == 0, 0.0, ref_loss), size)
+    close_grad(grad2, ref_grad * wd, terms * wd)
+    wide = torch.full((T, V + 3), 7.0, dtype=x.dtype, device="cuda")
+    args = dict(weight=w.cuda(), teacher_lse=None if lse is None else lse.cuda(), temperature=tau)
+    bcq.bcq_distill_fwd_bwd(x, z.cuda(), j.cuda(), dlogits=wide[:, 2:V + 2], **args)
+    assert torch.equal(wide[:, 2:V + 2], grad2) and (wide[:, :2] == 7).all() and (wide[:, V + 2:] == 7).all()
+    bcq.bcq_distill_fwd_bwd(x, z.cuda(), j.cuda(), dlogits=x, **args)
+    assert torch.equal(x, grad2)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("V", [40, 9001, 70001])
+def test_distill_unusual_lists(V, rest):
+    """Indices that stand twice, teacher values of -inf, students far from the teacher, probabilities 0, bad indices."""
+    T, k, tau = 8, 16, 1.5
+    x = table(T, V, "f32", seed=V)
+    z, j, lse = teacher(x, k, tau)
+    z, j = z.clone(), j.clone()
+    j[0, 3] = j[0, 9] = j[0, 1]
+    z[1, 4:] = -INF
+    x[2] -= 400.0 * torch.isin(torch.arange(V), j[2].long()).float().cuda()  # the listed entries are unlikely
+    x[3] += 300.0 * torch.isin(torch.arange(V), j[3].long()).float().cuda()  # the others are
+    x[4, j[4, 5].long()] = -INF                                           # a listed entry is masked
+    x[5] = -INF                                                           # a masked row
+    z[6] = -INF
+    lse = lse if rest else None
+    if rest:
+        lse[7] += 3.0                                                     # a large rest
+    ref_loss, ref_grad, terms, size = distill_reference(x, z, j, lse, tau)
+    w = torch.ones((T,))
+    loss, grad, (loss2, grad2) = run_distill(x, z, j, lse, tau, w)
+    for a, b in ((loss, grad), (loss2, grad2)):
+        close(a, ref_loss, size)
+        close_grad(b, ref_grad, terms)
+    j[0, 2], j[1, 0] = V, 2 ** 31 - 1
+    again = run_distill(x, z, j, lse, tau, w)
+    for a, b, before in ((again[0], again[1], grad), (*again[2], grad2)):
+        assert torch.isnan(a[:2]).all() and torch.isnan(b[:2]).all()
+        assert torch.equal(b[2:], before[2:]) and not torch.isnan(a[2:]).any()
+
+
+def test_list_of_the_whole_vocabulary():
+    T, V, tau = 3, 100, 1.0
+    x = table(T, V, "f32")
+    z, j, lse = teacher(x, V, tau)
+    ref_loss, ref_grad, terms, size = distill_reference(x, z, j, lse, tau)
+    loss, grad, (loss2, grad2) = run_distill(x, z, j, lse, tau, torch.ones((T,)))
+    close(loss, ref_loss, size)
+    close(loss2, ref_loss, size)
+    close_grad(grad, ref_grad, terms)
+    close_grad(grad2, ref_grad, terms)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(9, 300), (9, 20011), (9, 150001), (600, 20011)])
+def test_masks_and_special_values(T, V, dtype):
+    """-inf and lowest-value masks, rows left empty, constant rows, NaN and infinities that stay in their rows."""
+    x = table(T, V, dtype, seed=V)
+    lowest = torch.finfo(x.dtype).min
+    keep = torch.rand((V,), generator=torch.Generator().manual_seed(4)) < 0.05
+    keep[V // 2] = True
+    x[0, ~keep.cuda()] = -INF
+    x[1, ~keep.cuda()] = lowest
+    x[2] = -INF
+    x[3] = lowest
+    x[4] = 0.0
+    x[4, V // 3:] = -0.0
+    x[5] = -INF
+    x[5, V - 1] = 3.0
+    x[6, V // 2] = float("nan")
+    x[7, V - 2] = INF
+    tok = torch.full((T,), V // 2)
+    tok[5] = V - 1
+    k = 12
+    dev = tok.cuda()
+    out = bcq.bcq_logprobs_fwd(x, dev, k=k, entropy=True, lse=True, stats=True)
+    logq, logp, H, lse = (t.cpu() for t in reference(x, tok, 1.0))
+    index = best(x, k)
+    poisoned = torch.zeros((T,), dtype=torch.bool)
+    poisoned[6:8] = True
+    assert torch.equal(out.top_index.cpu()[~poisoned], index[~poisoned])
+    assert torch.equal(out.top_index.cpu()[poisoned], index[poisoned])
+    for got in (out.logp, out.entropy, out.lse, out.top_logp):
+        assert torch.isnan(got.cpu()[poisoned]).all()
+    live = ~poisoned
+    close(out.logp.cpu()[live], logp[live])
+    close(out.entropy.cpu()[live], H[live], 1.0 + math.log(V) + H[live])
+    close(out.lse.cpu()[live], lse[live])
+    close(out.top_logp.cpu()[live], logq.gather(1, index.long().clamp(min=0))[live])
+    g = torch.ones((T,))
+    dx = bcq.bcq_logprobs_bwd(x, out.stats, dev, g.cuda(), out.entropy, (0.1 * g).cuda()).cpu()
+    assert torch.isnan(dx[poisoned]).all() and not torch.isnan(dx[live]).any()
+    assert (dx[2] == 0).all()
+    q = torch.exp(logq)
+    unit = torch.zeros_like(q).scatter_(1, tok[:, None], 1.0)
+    logq0 = torch.where(q == 0, 0.0, logq)
+    ref = unit - q - 0.1 * q * torch.where(q == 0, 0.0, logq0 + H[:, None])
+    size = unit + q + 0.1 * q * (logq0.abs() + H[:, None])
+    ref[2] = 0.0
+    close_grad(dx[live], ref[live], size[live])
+    z, j = torch.zeros((T, 3)), torch.tensor([[V // 2, 1, V - 1]] * T, dtype=torch.int32)
+    for lse_t in (None, torch.full((T,), 2.0)):
+        loss, grad, (loss2, grad2) = run_distill(x, z, j, lse_t, 1.0, g)
+        ref_loss, ref_grad, terms, size = (t.cpu() for t in distill_reference(x, z, j, lse_t, 1.0))
+        for a, b in ((loss, grad), (loss2, grad2)):
+            assert torch.isnan(a.cpu()[poisoned]).all() and torch.isnan(b.cpu()[poisoned]).all()
+            close(a.cpu()[live], ref_loss[live], size[live])
+            close_grad(b[live.cuda()], ref_grad[live], terms[live])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [50, 777, 30011, 200003])
+@pytest.mark.parametrize("pattern", ["constant", "two", "rising", "falling", "period", "few", "nan"])
+def test_top_of_ties_and_orders(pattern, V, dtype):
+    """Alternatives where many entries are equal, sorted, gathered in few places or missing."""
+    i = torch.arange(V, dtype=torch.float64)
+    x = {"constant": torch.full((V,), 1.5), "two": (i * 7919 % 13 == 0).double(), "rising": i / 64, "falling": -i / 64,
+         "period": torch.where(i % 4096 < 16, i / 1024, -i), "few": torch.where(i % (V // 6) == 3, i % 5, -INF),
+         "nan": torch.where(i % (V // 6) == 3, i % 5, float("nan"))}[pattern]
+    x = torch.stack([x, x.flip(0)]).to(DTYPES[dtype]).cuda()
+    for k in (1, 12, 50, 128):
+        out = bcq.bcq_logprobs_fwd(x, k=k)
+        index = best(x, k)
+        assert torch.equal(out.top_index.cpu(), index), k
+        got = out.top_logit.cpu()
+        assert torch.equal(got, torch.where(index < 0, -INF, x.float().cpu().gather(1, index.long().clamp(min=0))))
+        assert torch.isnan(out.top_logp).all() == (pattern == "nan")
+
+
+def test_tokens_out_of_range_and_skipped_rows():
+    T, V = 5, 3001
+    x = table(T, V, "bf16")
+    x[2] = float("nan")                                  # never read: it has no token
+    tok = torch.tensor([3, V, -1, 2 ** 40, V - 1], device="cuda")
+    out = bcq.bcq_logprobs_fwd(x, tok, stats=True)
+    assert torch.isnan(out.logp).tolist() == [False, True, False, True, False] and out.logp[2] == 0
+    g = torch.tensor([1.0, 1.0, 1.0, 0.0, 0.0], device="cuda")
+    dx = bcq.bcq_logprobs_bwd(x, out.stats, tok, g)
+    assert torch.isnan(dx[1]).all() and not torch.isnan(dx[0]).any() and (dx[2:] == 0).all()
+
+
+def test_large_offsets():
+    """Rows that begin beyond 2^32 elements."""
+    stride, V, T = (1 << 31) + 3, 1003, 3  # rows aligned as those of the dense table
+    buf = torch.empty(((T - 1) * stride + V,), dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((T, V), (stride, 1))
+    src = table(T, V, "bf16", seed=8)
+    x.copy_(src)
+    tok = torch.tensor([5, 6, 7], device="cuda")
+    g = torch.ones((T,), device="cuda")
+    want = bcq.bcq_logprobs_fwd(src, tok, k=4, stats=True)
+    got = bcq.bcq_logprobs_fwd(x, tok, k=4, stats=True)
+    assert torch.equal(got.logp, want.logp) and torch.equal(got.top_index, want.top_index)
+    z, j, lse = (t.cuda() for t in teacher(src, 4, 1.0))
+    a = bcq.bcq_distill_fwd_bwd(src, z, j, teacher_lse=lse)
+    ref = bcq.bcq_logprobs_bwd(src, want.stats, tok, g)
+    assert torch.equal(bcq.bcq_distill_fwd_bwd(x, z, j, teacher_lse=lse)[1], a[1])
+    bcq.bcq_logprobs_bwd(x, got.stats, tok, g, dlogits=x)
+    assert torch.equal(x, ref)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_autograd(dtype):
+    """The differentiable forms: shapes with a batch, gradients that arrive expanded, unused outputs, accumulation."""
+    Bn, Sn, V = 2, 3, 501
+    x = table(Bn * Sn, V, dtype).reshape(Bn, Sn, V).requires_grad_(True)
+    tok = tokens_for(Bn * Sn, V).reshape(Bn, Sn).cuda()
+    logp, H = autograd.token_logprobs(x, tok, temperature=0.9, entropy=True)
+    assert logp.shape == H.shape == (Bn, Sn)
+    xd = x.detach().double().cpu().requires_grad_(True)
+    lq = torch.log_softmax(xd / 0.9, -1)
+    lp = torch.where(tok.cpu() < 0, 0.0, lq.gather(-1, tok.cpu().clamp(min=0)[..., None])[..., 0])
+    Hd = -(lq.exp() * lq).sum(-1)
+    tol = 1e-2 if dtype == "bf16" else 1e-5
+    for ours, theirs in ((logp.sum(), lp.sum()), (H.mean(), Hd.mean()), (logp.sum() - 0.2 * H.sum(), lp.sum() - 0.2 * Hd.sum())):
+        a, = torch.autograd.grad(ours, x, retain_graph=True)
+        b, = torch.autograd.grad(theirs, xd, retain_graph=True)
+        assert a.dtype == x.dtype and a.shape == x.shape
+        assert (a.double().cpu() - b).abs().max() <= tol * b.abs().max()
+    assert autograd.token_logprobs(x, tok)[1] is None
+    z, j, lse = teacher(x.detach().reshape(-1, V), 9, 2.0)
+    z, j, lse = z.reshape(Bn, Sn, 9).cuda(), j.reshape(Bn, Sn, 9).cuda(), lse.reshape(Bn, Sn).cuda()
+    loss = autograd.distill_loss(x, z, j, lse, temperature=2.0)
+    assert loss.shape == (Bn, Sn)
+    both, = torch.autograd.grad(loss.sum(), x)
+    ref = distill_reference(x.detach().reshape(-1, V), z.reshape(-1, 9).cpu(), j.reshape(-1, 9).cpu(), lse.reshape(-1).cpu(), 2.0)
+    close(loss.reshape(-1), ref[0], ref[3])
+    close_grad(both.reshape(-1, V), ref[1], ref[2])
+    # rows that are no view of a table, a transposed table
+    xt = x.detach()[:, :-1].transpose(0, 1).requires_grad_(True)
+    g1, = torch.autograd.grad(autograd.token_logprobs(xt, tok[:, :-1].T)[0].sum(), xt)
+    g2, = torch.autograd.grad(autograd.token_logprobs(x, tok)[0][:, :-1].sum(), x)
+    assert (g1.transpose(0, 1) - g2[:, :-1]).abs().max() <= tol * g2.abs().max()
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(autograd.token_logprobs(x, tok)[0].sum(), x, create_graph=True)[0].sum().backward()
+
+
+def test_gradients_against_differences():
+    """Central differences of the kernels' own values along random directions.  The step is 2^-6: the values' error 2^-18 (1 + 8)
+    over it is below 3e-3, the third-order term below step^2 |u|^3 <= 2.5e-4 * 30."""
+    T, V, step = 4, 40, 2.0 ** -6
+    x = table(T, V, "f32", scale=1.0)
+    tok = torch.tensor([1, 5, 39, 0], device="cuda")
+    z, j, lse = (t.cuda() for t in teacher(x, 6, 1.0))
+    ones = torch.ones((T,), device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+
+    def values(y):
+        out = bcq.bcq_logprobs_fwd(y, tok, entropy=True, stats=True)
+        return {"logp": out.logp, "entropy": out.entropy, "list": bcq.bcq_distill_fwd(y, z, j),
+                "rest": bcq.bcq_distill_fwd(y, z, j, lse)}, out
+
+    _, out = values(x)
+    grads = {"logp": bcq.bcq_logprobs_bwd(x, out.stats, tok, ones),
+             "entropy": bcq.bcq_logprobs_bwd(x, out.stats, entropy=out.entropy, dentropy=ones),
+             "list": bcq.bcq_distill_fwd_bwd(x, z, j)[1], "rest": bcq.bcq_distill_fwd_bwd(x, z, j, teacher_lse=lse)[1]}
+    for _ in range(5):
+        u = torch.randn((T, V), generator=gen, device="cuda")
+        up, down = values(x + step * u)[0], values(x - step * u)[0]
+        for name, dx in grads.items():
+            change = (up[name] - down[name]) / (2 * step)
+            assert ((dx * u).sum(1) - change).abs().max() <= 1e-2, name
+
+
+def test_graph_and_streams():
+    """Recorded into a graph and replayed between eager calls; used on a stream of its own."""
+    T, V, k = 40, 50257, 20
+    x = table(T, V, "bf16")
+    tok = tokens_for(T, V).cuda()
+    z, j, lse = (t.cuda() for t in teacher(x, k, 1.0))
+    outs = bcq.bcq_logprobs_fwd(x, tok, k=k, entropy=True, lse=True, stats=True)
+    loss, dx = bcq.bcq_distill_fwd_bwd(x, z, j, teacher_lse=lse)
+    n4 = bcq.logits_workspace_bytes(4, T, V, k, 1)
+    n6 = bcq.logits_workspace_bytes(6, T, V, k, 1)
+    ws4, ws6 = (torch.empty((max(n, 16),), dtype=torch.uint8, device="cuda") for n in (n4, n6))
+    fill = bcq.Logprobs(*(torch.empty_like(t) for t in outs))
+    loss2, dx2 = torch.empty_like(loss), torch.empty_like(dx)
+
+    def step():
+        bcq.bcq_logprobs_fwd(x, tok, k=k, out=fill, workspace=ws4)
+        bcq.bcq_distill_fwd_bwd(x, z, j, teacher_lse=lse, loss=loss2, dlogits=dx2, workspace=ws6)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for t in (*fill, loss2, dx2, ws4, ws6):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((*fill, loss2, dx2), (*outs, loss, dx)):
+            assert torch.equal(a, b)
+        bcq.bcq_logprobs_fwd(x, tok, k=3)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = bcq.bcq_distill_fwd_bwd(x, z, j, teacher_lse=lse)
+    side.synchronize()
+    assert torch.equal(again[0], loss) and torch.equal(again[1], dx)
+
+
+def test_refusals():
+    x = table(4, 100, "bf16")
+    tok = torch.zeros((4,), dtype=torch.int64, device="cuda")
+    z, j = torch.zeros((4, 3), device="cuda"), torch.zeros((4, 3), dtype=torch.int32, device="cuda")
+    for bad in (x.cpu(), x.half(), x[0], x.T, x[:, ::2], x[:1].expand(4, 100)):
+        with pytest.raises(ValueError):
+            bcq.bcq_logprobs_fwd(bad, k=1)
+        with pytest.raises(ValueError):
+            bcq.bcq_distill_fwd_bwd(bad, z, j)
+    for bad in (tok.int(), tok[:3], tok.cpu()):
+        with pytest.raises(ValueError):
+            bcq.bcq_logprobs_fwd(x, bad)
+    for zz, jj in ((z.bfloat16(), j), (z, j.long()), (z[:, :2], j), (z[:3], j[:3]), (z, j.cpu())):
+        with pytest.raises(ValueError):
+            bcq.bcq_distill_fwd(x, zz, jj)
+    with pytest.raises(ValueError):
+        bcq.bcq_distill_fwd_bwd(x, z, j, dlogits=x.float())
+    with pytest.raises(ValueError):
+        bcq.bcq_distill_fwd_bwd(x, z, j, weight=torch.ones((4,), dtype=torch.float64, device="cuda"))
+    for call in (lambda: bcq.bcq_logprobs_fwd(x), lambda: bcq.bcq_logprobs_fwd(x, k=129),
+                 lambda: bcq.bcq_logprobs_fwd(x, tok, temperature=0.0),
+                 lambda: bcq.bcq_distill_fwd(x, z[:, :0].contiguous(), j[:, :0].contiguous()),
+                 lambda: bcq.bcq_logprobs_bwd(x, torch.zeros((4, 2), device="cuda"))):
+        with pytest.raises(bcq.BcqError):
+            call()
+    empty = x[:0]
+    assert bcq.bcq_logprobs_fwd(empty, tok[:0], k=2).top_index.shape == (0, 2)
+    loss, dx = bcq.bcq_distill_fwd_bwd(empty, z[:0], j[:0])
+    assert loss.shape == (0,) and dx.shape == (0, 100)
