@@ -1,327 +1,1007 @@
 // Operators on logits: log probabilities of given tokens with entropy and the best alternatives, distillation from a
 // teacher's top logits, and their gradients.  Formulas and conventions: include/bcq.h.
 //
-// One workgroup takes one row and walks it once per quantity (maximum, sums, gradient; one walk per alternative).
+// A row is cut into chunks of whole 16-byte vectors (its unaligned ends belong to the first); one workgroup loads a chunk
+// into registers once, all loads in flight together, and takes everything from there: maximum and sums, the candidates
+// for the best alternatives, the gradient.  One chunk per row where rows alone fill the card; with few rows several, whose
+// partial results a second kernel joins.
 #include "../../include/bcq.h"
 
 #include "bcq_internal.h"
 
+#include <limits.h>
 #include <math.h>
 
 namespace bcq {
 
-constexpr int LG_THREADS = 256;
 constexpr float LG_LOG2E = 1.4426950408889634f;
 constexpr float LG_LN2 = 0.6931471805599453f;
-constexpr int LG_SEGMENT = 65536;  // columns whose list membership one bitmap holds
+constexpr int LG_MAX_THREADS = 1024;
+constexpr int LG_MAX_NV = 16;          // vectors per thread at most
+constexpr int LG_MAX_SPLITS = 64;      // chunks per row at most: a wave joins them, one per lane
+constexpr int LG_CANDIDATES = 1024;    // entries that are ranked against each other
+constexpr int LG_JOIN_CANDIDATES = 2048;
 
 __device__ __forceinline__ float lg_exp2(float v) { return __builtin_amdgcn_exp2f(v); }
+// The larger of numbers, NaN left out (fmaxf would first quieten its operands, an instruction each)
+__device__ __forceinline__ float lg_max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float lg_max2(float a, float b) { return lg_max3(a, b, b); }
 
 // A float as an unsigned number of the same order (-0 as +0); 0 is below every number.  NaN is not passed in.
 __device__ __forceinline__ uint32_t lg_key(float v) {
     const uint32_t u = __float_as_uint(v + 0.0f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
-
-template <typename V, typename F>
-__device__ __forceinline__ V lg_block_reduce(V v, F op, V* lds) {
-    const int tid = threadIdx.x;
-    __syncthreads();
-    lds[tid] = v;
-    __syncthreads();
-    for (int s = LG_THREADS / 2; s > 0; s >>= 1) {
-        if (tid < s) lds[tid] = op(lds[tid], lds[tid + s]);
-        __syncthreads();
-    }
-    return lds[0];
+__device__ __forceinline__ float lg_unkey(uint32_t key) {
+    return __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
 }
-__device__ __forceinline__ float lg_add(float a, float b) { return a + b; }
-__device__ __forceinline__ float lg_max(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ uint64_t lg_max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
+// value and index as one number: the larger value first, then the lower index
+__device__ __forceinline__ uint64_t lg_entry(float v, int index) { return ((uint64_t)lg_key(v) << 32) | (uint32_t)~index; }
 
-struct LogprobsOut {
-    float *logp, *entropy, *lse, *stats, *top_logit, *top_logp;
-    int32_t* top_index;
+// ---- reductions: over the 16 lanes of a row, and over a wave; every lane gets the result
+template <int CTRL>
+__device__ __forceinline__ float lg_move(float v) { return __uint_as_float(dpp_move<CTRL>(__float_as_uint(v))); }
+__device__ __forceinline__ float lg_row_max(float v) {
+    v = lg_max2(v, lg_move<DPP_XOR1>(v));
+    v = lg_max2(v, lg_move<DPP_XOR2>(v));
+    v = lg_max2(v, lg_move<DPP_HALF_MIRROR>(v));
+    return lg_max2(v, lg_move<DPP_MIRROR>(v));
+}
+__device__ __forceinline__ float lg_row_sum(float v) {
+    v += lg_move<DPP_XOR1>(v);
+    v += lg_move<DPP_XOR2>(v);
+    v += lg_move<DPP_HALF_MIRROR>(v);
+    return v + lg_move<DPP_MIRROR>(v);
+}
+__device__ __forceinline__ float lg_lane(float v, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)); }
+__device__ __forceinline__ float lg_wave_max(float v) {
+    v = lg_row_max(v);
+    return lg_max2(lg_max2(lg_lane(v, 0), lg_lane(v, 16)), lg_max2(lg_lane(v, 32), lg_lane(v, 48)));
+}
+__device__ __forceinline__ float lg_wave_sum(float v) {
+    v = lg_row_sum(v);
+    return (lg_lane(v, 0) + lg_lane(v, 16)) + (lg_lane(v, 32) + lg_lane(v, 48));
+}
+
+// Sums of a part of a row: S = sum 2^d, E = sum 2^d d, d = (x - m) c2, m the part's maximum (0 where it holds nothing).
+struct Part {
+    float m, S, E;
+};
+// the maximum as a shift
+__device__ __forceinline__ float lg_shift(float m) { return m == -INFINITY ? 0.f : m; }
+// log2 of the factor from shift m to shift M >= m; far below what a sum can feel it stays finite (products with E)
+__device__ __forceinline__ float lg_step(float m, float M, float c2) { return fmaxf((m - M) * c2, -16384.f); }
+// p's sums relative to the shift M
+template <bool ENT>
+__device__ __forceinline__ Part lg_reshift(Part p, float M, float c2) {
+    const float step = lg_step(p.m, M, c2), f = lg_exp2(step);
+    if constexpr (ENT) p.E = f * fmaf(step, p.S, p.E);
+    p.S *= f;
+    return p;
+}
+// over the lanes of a wave (m: the lane's raw maximum, -inf for none; its sums relative to lg_shift(m))
+template <bool ENT>
+__device__ __forceinline__ Part lg_wave_join(Part p, float c2) {
+    const float m = lg_wave_max(p.m);
+    p = lg_reshift<ENT>(p, lg_shift(m), c2);
+    p.S = lg_wave_sum(p.S);
+    if constexpr (ENT) p.E = lg_wave_sum(p.E);
+    p.m = m;
+    return p;
+}
+// over the first n <= 16 parts in LDS, by every wave
+template <bool ENT>
+__device__ __forceinline__ Part lg_parts_join(const Part* parts, int n, float c2) {
+    const int l = threadIdx.x & 15;
+    Part p = parts[l < n ? l : 0];
+    if (l >= n) p = Part{-INFINITY, 0.f, 0.f};
+    const float m = lg_row_max(p.m);
+    p = lg_reshift<ENT>(p, lg_shift(m), c2);
+    p.S = lg_row_sum(p.S);
+    if constexpr (ENT) p.E = lg_row_sum(p.E);
+    p.m = m;
+    return p;
+}
+
+// ---- a chunk of a row in registers ----------------------------------------------------------------------------------
+template <typename XT> struct LgVec;
+template <> struct LgVec<float> {
+    static constexpr int N = 4;
+    static constexpr uint32_t NONE = 0xFF800000u;  // -inf
+    __device__ static __forceinline__ float get(const uint32_t (&w)[4], int e) { return __uint_as_float(w[e]); }
+    __device__ static __forceinline__ void clear(uint32_t (&w)[4], uint32_t bits) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (bits & (1u << e)) w[e] = NONE;
+    }
+    __device__ static __forceinline__ uint32_t pack(const float (&v)[4], int u) { return __float_as_uint(v[u]); }
+    __device__ static __forceinline__ void quiet(uint32_t& w) {
+        if ((w & 0x7FFFFFFFu) > 0x7F800000u) w |= 0x00400000u;
+    }
+};
+template <> struct LgVec<bf16_t> {
+    static constexpr int N = 8;
+    static constexpr uint32_t NONE = 0xFF80FF80u;
+    __device__ static __forceinline__ float get(const uint32_t (&w)[4], int e) {
+        return __uint_as_float((e & 1) ? (w[e >> 1] & 0xFFFF0000u) : (w[e >> 1] << 16));
+    }
+    __device__ static __forceinline__ void clear(uint32_t (&w)[4], uint32_t bits) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (bits & (1u << (2 * u))) w[u] = (w[u] & 0xFFFF0000u) | 0xFF80u;
+            if (bits & (2u << (2 * u))) w[u] = (w[u] & 0xFFFFu) | 0xFF800000u;
+        }
+    }
+    __device__ static __forceinline__ uint32_t pack(const float (&v)[8], int u) {
+        uint32_t r;  // round to nearest even, NaN stays NaN
+        asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(v[2 * u]), "v"(v[2 * u + 1]));
+        return r;
+    }
+    __device__ static __forceinline__ void quiet(uint32_t& w) {
+        if ((w & 0x7FFFu) > 0x7F80u) w |= 0x0040u;
+        if ((w & 0x7FFF0000u) > 0x7F800000u) w |= 0x00400000u;
+    }
 };
 
+template <typename XT, int NV>
+struct LgChunk {
+    using Vec = LgVec<XT>;
+    uint32_t w[NV][4];
+    float edge;      // an entry before or behind the row's vectors (-inf for none), of the first threads of the first chunk
+    int edge_index;  // its column, -1 for none
+    int head;        // entries before the row's first whole vector
+    int first, n;    // the chunk's vectors
+
+    // chunk number `chunk` of `per` vectors of the row
+    __device__ __forceinline__ void load(const XT* row, int V, int chunk, int per) {
+        const int tid = threadIdx.x, threads = blockDim.x;
+        const int skip = (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(XT);
+        head = skip < V ? skip : V;
+        const int vectors = (V - head) / Vec::N;
+        first = chunk * per;
+        const int left = vectors - first;
+        n = left < per ? (left > 0 ? left : 0) : per;
+        if (n > 0) {
+            const char* base = reinterpret_cast<const char*>(row + head) + (int64_t)first * 16;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {  // lanes beyond the end repeat the last vector
+                const int j = i * threads + tid;
+                const uint4 q = *reinterpret_cast<const uint4*>(base + (uint32_t)(j < n ? j : n - 1) * 16u);
+                w[i][0] = q.x, w[i][1] = q.y, w[i][2] = q.z, w[i][3] = q.w;
+            }
+        }
+        edge_index = -1;
+        if (chunk == 0) {
+            const int tail = head + vectors * Vec::N;
+            const int i = tid < head ? tid : tail + (tid - head);
+            if (i < V) edge_index = i;
+        }
+        edge = edge_index >= 0 ? Elem<XT>::load(row + edge_index) : -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if ((i + 1) * threads > n && i * threads + tid >= n) w[i][0] = w[i][1] = w[i][2] = w[i][3] = Vec::NONE;
+    }
+    __device__ __forceinline__ int column(int i, int e) const {
+        return head + (first + i * (int)blockDim.x + (int)threadIdx.x) * Vec::N + e;
+    }
+    __device__ __forceinline__ bool any(int i) const { return i * (int)blockDim.x < n; }  // the same in all lanes
+
+    __device__ __forceinline__ float max() const {
+        float m = edge;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (any(i))
+#pragma unroll
+                for (int e = 0; e < Vec::N; e += 2) m = lg_max3(m, Vec::get(w[i], e), Vec::get(w[i], e + 1));
+        return lg_max2(m, -INFINITY);
+    }
+    // NaN made quiet: the maximum instructions leave those out and take a signalling one for the result
+    __device__ __forceinline__ void quiet() {
+        if (edge != edge) edge = NAN;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (any(i))
+#pragma unroll
+                for (int u = 0; u < 4; ++u) Vec::quiet(w[i][u]);
+    }
+    // sums relative to the thread's own maximum
+    template <bool ENT>
+    __device__ __forceinline__ Part sums(float m, float c2) const {
+        const float shift = lg_shift(m);
+        Part p{m, 0.f, 0.f};
+        float S2 = 0.f;
+        auto one = [&](float x, float& S) {
+            const float d = (x - shift) * c2, e = lg_exp2(d);
+            S += e;
+            if constexpr (ENT) p.E = fmaf(e, lg_max2(d, -16384.f), p.E);
+        };
+        one(edge, p.S);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (any(i))
+#pragma unroll
+                for (int e = 0; e < Vec::N; e += 2) {
+                    one(Vec::get(w[i], e), p.S);
+                    one(Vec::get(w[i], e + 1), S2);
+                }
+        p.S += S2;
+        return p;
+    }
+    // f(value, column) of every entry of this thread for which keep(value)
+    template <typename K, typename F>
+    __device__ __forceinline__ void each(K keep, F f) const {
+        if (edge_index >= 0 && keep(edge)) f(edge, edge_index);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (any(i) && i * (int)blockDim.x + (int)threadIdx.x < n) {
+                float m = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < Vec::N; e += 2) m = lg_max3(m, Vec::get(w[i], e), Vec::get(w[i], e + 1));
+                if (keep(m))
+#pragma unroll
+                    for (int e = 0; e < Vec::N; ++e) {
+                        const float x = Vec::get(w[i], e);
+                        if (keep(x)) f(x, column(i, e));
+                    }
+            }
+    }
+    // number of entries of this thread for which keep(value, column)
+    template <typename K>
+    __device__ __forceinline__ uint32_t count(K keep) const {
+        uint32_t c = edge_index >= 0 && keep(edge, edge_index);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (any(i) && i * (int)blockDim.x + (int)threadIdx.x < n)
+#pragma unroll
+                for (int e = 0; e < Vec::N; ++e) c += keep(Vec::get(w[i], e), column(i, e)) ? 1u : 0u;
+        return c;
+    }
+    // row[column] = f(value) for every entry of the chunk
+    template <typename F>
+    __device__ __forceinline__ void store(XT* row, F f) const {
+        if (edge_index >= 0) Elem<XT>::store(row + edge_index, f(edge));
+        char* base = reinterpret_cast<char*>(row + head) + (int64_t)first * 16;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (any(i)) {
+                float v[Vec::N];
+#pragma unroll
+                for (int e = 0; e < Vec::N; ++e) v[e] = f(Vec::get(w[i], e));
+                uint32_t q[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) q[u] = Vec::pack(v, u);
+                const int j = i * (int)blockDim.x + (int)threadIdx.x;
+                // the gradient's rows may be aligned otherwise than the logits'
+                if (j < n) __builtin_memcpy(base + (uint32_t)j * 16u, q, 16);
+            }
+    }
+};
+
+// zeros over the whole row, by the workgroups of its chunks together
 template <typename XT>
-__global__ __launch_bounds__(LG_THREADS) void logprobs_kernel(const XT* __restrict__ x, int64_t stride, int V,
-                                                              const int64_t* __restrict__ tokens, float c, int k, LogprobsOut out) {
-    __shared__ float lds[LG_THREADS];
-    __shared__ uint64_t lds64[LG_THREADS];
-    const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x;
-    const XT* row = x + t * stride;
-    const float c2 = c * LG_LOG2E;
-    const int64_t token = tokens ? tokens[t] : -1;
-    if (token < 0 && !out.entropy && !out.lse && k == 0) {
-        if (tid == 0) {
-            if (out.logp) out.logp[t] = 0.f;
-            if (out.stats) out.stats[2 * t] = out.stats[2 * t + 1] = 0.f;
+__device__ __forceinline__ void lg_zero_row(XT* row, int V, int chunk, int chunks) {
+    const int skip = (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(XT);
+    const int head = skip < V ? skip : V, N = LgVec<XT>::N, vectors = (V - head) / N;
+    if (chunk == 0) {
+        const int tail = head + vectors * N, i = (int)threadIdx.x < head ? (int)threadIdx.x : tail + ((int)threadIdx.x - head);
+        if (i < V) Elem<XT>::store(row + i, 0.f);
+    }
+    uint4* base = reinterpret_cast<uint4*>(row + head);
+    for (int j = chunk * (int)blockDim.x + (int)threadIdx.x; j < vectors; j += chunks * (int)blockDim.x) base[j] = make_uint4(0, 0, 0, 0);
+}
+
+// ---- log probabilities ------------------------------------------------------------------------------------------------
+struct LogprobsArgs {
+    const void* x;
+    int64_t stride;
+    const int64_t* tokens;
+    float c;
+    int V, k, splits, per;  // per: vectors of a chunk
+    int64_t row0;           // of this launch
+    float *logp, *entropy, *lse, *stats, *top_logit, *top_logp;
+    int32_t* top_index;
+    float4* parts;    // [T][splits] of a split row
+    uint64_t* lists;  // [T][splits][k]
+};
+
+// The row's values but the alternatives', by one thread
+template <typename XT>
+__device__ __forceinline__ void lg_write_row(const LogprobsArgs& a, int64_t t, int64_t token, Part p, float l2) {
+    const float m = lg_shift(p.m);
+    const bool none = p.S == 0.f;
+    if (a.logp) {
+        float v = 0.f;
+        if (token >= a.V) v = NAN;
+        else if (token >= 0)
+            v = none ? -INFINITY : (Elem<XT>::load(static_cast<const XT*>(a.x) + t * a.stride + token) - m) * a.c - l2 * LG_LN2;
+        a.logp[t] = v;
+    }
+    if (a.entropy) a.entropy[t] = none ? 0.f : (l2 - p.E / p.S) * LG_LN2;
+    if (a.lse) a.lse[t] = none ? -INFINITY : m * a.c + l2 * LG_LN2;
+    if (a.stats) {
+        a.stats[2 * t] = m;
+        a.stats[2 * t + 1] = l2;
+    }
+}
+// one of the k alternatives (entry 0: there is none)
+__device__ __forceinline__ void lg_write_top(const LogprobsArgs& a, int64_t t, int rank, uint64_t entry, Part p, float l2) {
+    const float v = entry ? lg_unkey((uint32_t)(entry >> 32)) : -INFINITY;
+    const int64_t at = t * a.k + rank;
+    if (a.top_index) a.top_index[at] = entry ? (int32_t)~(uint32_t)entry : -1;
+    if (a.top_logit) a.top_logit[at] = v;
+    if (a.top_logp) a.top_logp[at] = p.S == 0.f ? -INFINITY : (v - lg_shift(p.m)) * a.c - l2 * LG_LN2;
+}
+
+// put(rank, entry) for the k first of the n entries in `list` by rank, and entry 0 for ranks beyond n
+template <typename F>
+__device__ __forceinline__ void lg_rank(const uint64_t* list, int n, int k, F put) {
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const uint64_t mine = list[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
+        if (rank < k) put(rank, mine);
+    }
+    for (int r = n + (int)threadIdx.x; r < k; r += blockDim.x) put(r, (uint64_t)0);
+}
+
+struct TopLds {
+    float max[LG_MAX_THREADS];  // of every thread
+    uint64_t list[LG_CANDIDATES];
+    uint32_t counts[2][16];
+    int n;
+};
+
+// The candidates for a chunk's k best in lds.list, and their number.  At least k threads have a maximum that reaches the k-th
+// largest of the threads' maxima, so that value is a lower bound of the k-th entry, and few entries exceed it: of n random
+// entries over 832 threads about k + k^2 / 1700.  The bound only has to be low enough, so its search stops early.
+// Called by all threads after lds.max is written and a barrier; lds.n is 0.
+template <typename XT, int NV>
+__device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>& chunk, float tm, int k) {
+    const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+    uint32_t key[16];
+    float most = -INFINITY, least = -INFINITY;  // of the maxima; the least one's negative
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        key[v] = 0;
+        if (v < waves) {
+            const float x = lds.max[v * 64 + lane];
+            key[v] = lg_key(x);
+            most = lg_max2(most, x);
+            least = lg_max2(least, -x);
+        }
+    }
+    uint32_t low = lg_key(-INFINITY);
+    uint32_t high = lg_key(lg_wave_max(most)) + 1;  // no entry reaches it
+    if ((int)blockDim.x >= k) {
+        low = lg_key(-lg_wave_max(least));
+        uint32_t reach = blockDim.x, above = high;
+        while (above - low > 1 && (int)reach > k + 8 + k / 4) {
+            const uint32_t mid = low + (above - low) / 2;
+            uint32_t c = 0;
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (v < waves) c += (uint32_t)__popcll(__ballot(key[v] >= mid));
+            if ((int)c >= k) low = mid, reach = c;
+            else above = mid;
+        }
+    }
+    const float bound = lg_unkey(low);
+    if (tm >= bound)
+        chunk.each([&](float x) { return x >= bound; },
+                   [&](float x, int index) {
+                       const int at = atomicAdd(&lds.n, 1);
+                       if (at < LG_CANDIDATES) lds.list[at] = lg_entry(x, index);
+                   });
+    __syncthreads();
+    int n = lds.n;
+    if (n <= LG_CANDIDATES) return n;
+
+    // Too many: many equal entries (masked rows), or rows whose large entries meet in few threads.  Exact search for the
+    // k-th value by halving, counting entries in registers, then for the column up to which entries of that value count.
+    __syncthreads();
+    uint32_t greater = 0;  // entries that reach `high`
+    int turn = 0;
+    auto total = [&](uint32_t c) {
+        c = wave_sum(c);
+        if (lane == 0) lds.counts[turn & 1][threadIdx.x >> 6] = c;
+        __syncthreads();
+        uint32_t s = 0;
+        for (int v = 0; v < waves; ++v) s += lds.counts[turn & 1][v];
+        ++turn;
+        return s;
+    };
+    uint32_t reach = (uint32_t)n;  // entries that reach `low`
+    while (high - low > 1) {
+        const uint32_t mid = low + (high - low) / 2;
+        const float at = lg_unkey(mid);
+        const uint32_t c = total(chunk.count([&](float x, int) { return x >= at; }));
+        if ((int)c >= k) low = mid, reach = c;
+        else high = mid, greater = c;
+    }
+    const float value = lg_unkey(low);
+    int last = INT_MAX;
+    if (reach > LG_CANDIDATES) {
+        int below = -1;  // greater + entries of the value up to `below` < k; up to `last` >= k
+        last = BCQ_LOGITS_MAX_V;
+        while (last - below > 1) {
+            const int mid = below + (last - below) / 2;
+            const uint32_t c = total(chunk.count([&](float x, int index) { return x == value && index <= mid; }));
+            if ((int)(greater + c) >= k) last = mid;
+            else below = mid;
+        }
+    }
+    if (threadIdx.x == 0) lds.n = 0;
+    __syncthreads();
+    chunk.each([&](float x) { return x >= value; },
+               [&](float x, int index) {
+                   if (x > value || index <= last) {
+                       const int at = atomicAdd(&lds.n, 1);
+                       if (at < LG_CANDIDATES) lds.list[at] = lg_entry(x, index);
+                   }
+               });
+    __syncthreads();
+    n = lds.n;
+    return n < LG_CANDIDATES ? n : LG_CANDIDATES;
+}
+
+template <typename XT, int NV, bool ENT, bool TOP>
+__global__ __launch_bounds__(LG_MAX_THREADS) void logprobs_kernel(LogprobsArgs a) {
+    __shared__ Part parts[16];
+    __shared__ TopLds top;
+    const int64_t t = a.row0 + blockIdx.x / (uint32_t)a.splits;
+    const int chunk_number = (int)(blockIdx.x % (uint32_t)a.splits);
+    const int tid = threadIdx.x, wave = tid >> 6, waves = blockDim.x >> 6;
+    const float c2 = a.c * LG_LOG2E;
+    const int64_t token = a.tokens ? a.tokens[t] : -1;
+    if (!ENT && !TOP && token < 0 && !a.lse) {  // nothing of this row is wanted
+        if (tid == 0 && chunk_number == 0) {
+            if (a.logp) a.logp[t] = 0.f;
+            if (a.stats) a.stats[2 * t] = a.stats[2 * t + 1] = 0.f;
         }
         return;
     }
-    float m = -INFINITY;
-    for (int i = tid; i < V; i += LG_THREADS) m = fmaxf(m, Elem<XT>::load(row + i));
-    m = lg_block_reduce(m, lg_max, lds);
-    if (m == -INFINITY) m = 0.f;
-    float S = 0.f, E = 0.f;
-    for (int i = tid; i < V; i += LG_THREADS) {
-        const float d = (Elem<XT>::load(row + i) - m) * c2, e = lg_exp2(d);
-        S += e;
-        E += e * fmaxf(d, -1e4f);
+    LgChunk<XT, NV> chunk;
+    chunk.load(static_cast<const XT*>(a.x) + t * a.stride, a.V, chunk_number, a.per);
+    float tm = chunk.max();
+    Part p = lg_wave_join<ENT>(chunk.template sums<ENT>(tm, c2), c2);
+    if ((tid & 63) == 0) parts[wave] = p;
+    if constexpr (TOP) {
+        top.max[tid] = tm;
+        if (tid == 0) top.n = 0;
     }
-    S = lg_block_reduce(S, lg_add, lds);
-    E = lg_block_reduce(E, lg_add, lds);
-    const float l2 = log2f(S);  // -inf: nothing left
+    __syncthreads();
+    p = lg_parts_join<ENT>(parts, waves, c2);
+    const bool whole = a.splits == 1;
+    const float l2 = whole ? log2f(p.S) : 0.f;
     if (tid == 0) {
-        if (out.logp) {
-            float v = 0.f;
-            if (token >= V) v = NAN;
-            else if (token >= 0) v = S == 0.f ? -INFINITY : (Elem<XT>::load(row + token) - m) * c - l2 * LG_LN2;
-            out.logp[t] = v;
-        }
-        if (out.entropy) out.entropy[t] = S == 0.f ? 0.f : (l2 - E / S) * LG_LN2;
-        if (out.lse) out.lse[t] = S == 0.f ? -INFINITY : m * c + l2 * LG_LN2;
-        if (out.stats) {
-            out.stats[2 * t] = m;
-            out.stats[2 * t + 1] = l2;
-        }
+        if (whole) lg_write_row<XT>(a, t, token, p, l2);
+        else a.parts[t * a.splits + chunk_number] = make_float4(p.m, p.S, p.E, 0.f);
     }
-    uint64_t below = ~(uint64_t)0;
-    for (int r = 0; r < k; ++r) {
-        uint64_t best = 0;
-        for (int i = tid; i < V; i += LG_THREADS) {
-            const float v = Elem<XT>::load(row + i);
-            if (v == v) {
-                const uint64_t key = ((uint64_t)lg_key(v) << 32) | (uint32_t)~i;
-                if (key < below) best = lg_max64(best, key);
-            }
+    if constexpr (TOP) {
+        if (p.S != p.S) {
+            chunk.quiet();
+            tm = chunk.max();
+            top.max[tid] = tm;
+            __syncthreads();
         }
-        best = lg_block_reduce(best, lg_max64, lds64);
-        below = best;
-        if (tid == 0) {
-            const int i = best ? (int)~(uint32_t)best : -1;
-            const float v = best ? Elem<XT>::load(row + i) : -INFINITY;
-            if (out.top_index) out.top_index[t * k + r] = i;
-            if (out.top_logit) out.top_logit[t * k + r] = v;
-            if (out.top_logp) out.top_logp[t * k + r] = S == 0.f ? -INFINITY : (v - m) * c - l2 * LG_LN2;
+        const int n = lg_candidates<XT, NV>(top, chunk, tm, a.k);
+        if (whole) lg_rank(top.list, n, a.k, [&](int rank, uint64_t entry) { lg_write_top(a, t, rank, entry, p, l2); });
+        else {
+            uint64_t* list = a.lists + (t * a.splits + chunk_number) * a.k;
+            lg_rank(top.list, n, a.k, [&](int rank, uint64_t entry) { list[rank] = entry; });
         }
     }
 }
 
-template <typename XT>
-__global__ __launch_bounds__(LG_THREADS) void logprobs_bwd_kernel(const XT* x, int64_t stride, int V,
-                                                                  const int64_t* __restrict__ tokens, float c,
-                                                                  const float* __restrict__ stats, const float* __restrict__ dlogp,
-                                                                  const float* __restrict__ entropy,
-                                                                  const float* __restrict__ dentropy, XT* dx, int64_t dstride) {
-    const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x;
-    const XT* row = x + t * stride;
-    XT* drow = dx + t * dstride;
-    const int64_t token = tokens ? tokens[t] : -1;
-    float g = token >= 0 ? dlogp[t] : 0.f;
-    const float h = dentropy ? dentropy[t] : 0.f;
-    const float m = stats[2 * t], l2 = stats[2 * t + 1];
+// Joins the chunks of a row: one workgroup per row
+template <typename XT, bool ENT, bool TOP>
+__global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobsArgs a) {
+    __shared__ uint64_t list[TOP ? LG_JOIN_CANDIDATES : 1];
+    __shared__ int count;
+    const int64_t t = a.row0 + blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const float c2 = a.c * LG_LOG2E;
+    const int64_t token = a.tokens ? a.tokens[t] : -1;
+    if (!ENT && !TOP && token < 0 && !a.lse) return;
+    const float4 f = lane < a.splits ? a.parts[t * a.splits + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    const Part p = lg_wave_join<ENT>(Part{f.x, f.y, f.z}, c2);
+    const float l2 = log2f(p.S);
+    if (tid == 0) lg_write_row<XT>(a, t, token, p, l2);
+    if constexpr (TOP) {
+        // The first ceil(k / splits) entries of every list are k together: the least of their last ones is a lower bound.
+        const uint64_t* lists = a.lists + t * a.splits * a.k;
+        const int deep = (a.k + a.splits - 1) / a.splits;
+        uint64_t bound = lane < a.splits ? lists[lane * a.k + deep - 1] : ~(uint64_t)0;
+        for (int s = 1; s < 64; s *= 2) {
+            const uint64_t other = __shfl_xor((unsigned long long)bound, s);
+            bound = other < bound ? other : bound;
+        }
+        if (bound == 0) bound = 1;  // entries that are missing
+        if (tid == 0) count = 0;
+        __syncthreads();
+        for (int i = tid; i < a.splits * a.k; i += 256) {
+            const uint64_t entry = lists[i];
+            if (entry >= bound) list[atomicAdd(&count, 1)] = entry;
+        }
+        __syncthreads();
+        lg_rank(list, count, a.k, [&](int rank, uint64_t entry) { lg_write_top(a, t, rank, entry, p, l2); });
+    }
+}
+
+struct LogprobsBwdArgs {
+    const void* x;
+    int64_t stride;
+    const int64_t* tokens;
+    const float *stats, *dlogp, *entropy, *dentropy;
+    float c;
+    int V, splits, per;
+    int64_t row0;
+    void* dx;
+    int64_t dstride;
+};
+
+template <typename XT, int NV, bool ENT>
+__global__ __launch_bounds__(256) void logprobs_bwd_kernel(LogprobsBwdArgs a) {
+    const int64_t t = a.row0 + blockIdx.x / (uint32_t)a.splits;
+    const int chunk_number = (int)(blockIdx.x % (uint32_t)a.splits);
+    const int V = a.V;
+    const float c = a.c;
+    const XT* row = static_cast<const XT*>(a.x) + t * a.stride;
+    XT* drow = static_cast<XT*>(a.dx) + t * a.dstride;
+    const int64_t token = a.tokens ? a.tokens[t] : -1;
+    float g = token >= 0 ? a.dlogp[t] : 0.f;
+    const float h = ENT ? a.dentropy[t] : 0.f;
+    const float m = a.stats[2 * t], l2 = a.stats[2 * t + 1];
     if ((g == 0.f && h == 0.f) || l2 == -INFINITY) {
-        for (int i = tid; i < V; i += LG_THREADS) Elem<XT>::store(drow + i, 0.f);
+        lg_zero_row(drow, V, chunk_number, a.splits);
         return;
     }
     if (token >= V) g = NAN;
+    LgChunk<XT, NV> chunk;
+    chunk.load(row, V, chunk_number, a.per);
     const float c2 = c * LG_LOG2E;
-    // dx = q (A + B ln2 log2 q) with log2 q = (x - m) c2 - l2
-    const float A = -c * (g + (h != 0.f ? h * entropy[t] : 0.f)), B = -c * h * LG_LN2;
-    for (int i = tid; i < V; i += LG_THREADS) {
-        const float d = (Elem<XT>::load(row + i) - m) * c2 - l2, q = lg_exp2(d);
-        float v = q * (A + B * fmaxf(d, -1e4f));
-        if (i == token) v += c * g;
-        Elem<XT>::store(drow + i, v);
+    // the token's entry is written once more, by the workgroup that has its chunk
+    int mine = -1;
+    float at = 0.f;
+    if (threadIdx.x == 0 && token >= 0 && token < V) {
+        const int v = (int)token < chunk.head ? -1 : ((int)token - chunk.head) / LgVec<XT>::N;
+        const bool edge = v < 0 || v >= (V - chunk.head) / LgVec<XT>::N;
+        if (edge ? chunk_number == 0 : (v >= chunk.first && v < chunk.first + chunk.n)) {
+            mine = (int)token;
+            at = Elem<XT>::load(row + token);
+        }
     }
+    // dx = q (A + B log2 q) with log2 q = (x - m) c2 - l2
+    const float A = -c * (g + (ENT && h != 0.f ? h * a.entropy[t] : 0.f)), B = -c * h * LG_LN2;
+    auto value = [&](float v) {
+        const float d = (v - m) * c2 - l2, q = lg_exp2(d);
+        if constexpr (ENT) return q * fmaf(B, lg_max2(d, -16384.f), A);
+        else return q * A;
+    };
+    if (a.x == a.dx) __syncthreads();  // `at` is read before its column is overwritten
+    chunk.store(drow, value);
+    __syncthreads();
+    if (mine >= 0) Elem<XT>::store(drow + mine, value(at) + c * g);
 }
 
 // ---- distillation -----------------------------------------------------------------------------------------------
-// The teacher's side of a row and the student's logits at the list, one entry per thread (k <= LG_THREADS / 2).
-struct ListLds {
-    int index[BCQ_LOGITS_MAX_K];
-    double p[BCQ_LOGITS_MAX_K], lp[BCQ_LOGITS_MAX_K];
-    float s[BCQ_LOGITS_MAX_K];
-    double sum[4];  // sum of p; sum of p ln p; entries; invalid entries
+struct DistillArgs {
+    const void* x;
+    int64_t stride;
+    const float* top_logit;
+    const int32_t* top_index;
+    const float* teacher_lse;
+    const float* weight;  // or the gradient of the loss
+    float c;
+    int V, k, splits, per;
+    int64_t row0;
+    float *loss, *stats;
+    float4* parts;
+    void* dx;
+    int64_t dstride;
 };
 
-template <typename XT>
-__device__ void lg_load_list(ListLds& L, const XT* row, int V, const float* __restrict__ z, const int32_t* __restrict__ index,
-                             int k, const float* __restrict__ teacher_lse, double c) {
-    const int tid = threadIdx.x;
-    __syncthreads();
-    if (tid < k) {
-        L.index[tid] = index[tid];
-        L.lp[tid] = (double)z[tid] * c;
-        L.s[tid] = L.index[tid] >= 0 && L.index[tid] < V ? Elem<XT>::load(row + L.index[tid]) : -INFINITY;
+// The teacher's side of a row and the student's logits at the list.
+struct ListLds {
+    int index[BCQ_LOGITS_MAX_K];
+    float s[BCQ_LOGITS_MAX_K];
+    float p[BCQ_LOGITS_MAX_K];  // the teacher's probability of the entry's index (of all entries with this index)
+    double P, H, U;             // sum of p; sum of p ln p; sum of p (s - m) c
+    float m, S;                 // the listed entries' maximum and sum, every index once
+    int distinct, bad;          // listed indices; whether one is out of range
+};
+
+__device__ __forceinline__ double lg_wave_max(double v) {
+    for (int s = 1; s < 64; s *= 2) {
+        const double o = __shfl_xor(v, s);
+        v = o > v || o != o ? o : v;
     }
-    __syncthreads();
-    if (tid == 0) {
-        double top = -INFINITY, sum = 0.0;
-        for (int i = 0; i < k; ++i)
-            if (L.index[i] >= 0) top = L.lp[i] > top || L.lp[i] != L.lp[i] ? L.lp[i] : top;
+    return v;
+}
+
+// By the first wave alone, two entries a lane; the caller's barrier follows.
+template <typename XT>
+__device__ __forceinline__ void lg_load_list(ListLds& L, const DistillArgs& a, int64_t t) {
+    const int lane = threadIdx.x;
+    const XT* row = static_cast<const XT*>(a.x) + t * a.stride;
+    const float* z = a.top_logit + t * a.k;
+    const int32_t* index = a.top_index + t * a.k;
+    const float c2 = a.c * LG_LOG2E;
+    int j[2];
+    double lp[2], p[2];
+    float s[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int i = lane + 64 * u;
+        j[u] = i < a.k ? index[i] : -1;
+        lp[u] = j[u] >= 0 ? (double)z[i] * a.c : -INFINITY;
+        s[u] = j[u] >= 0 && j[u] < a.V ? Elem<XT>::load(row + j[u]) : -INFINITY;
+        L.index[i] = j[u];
+        L.s[i] = s[u];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    double norm = a.teacher_lse ? (double)a.teacher_lse[t] : 0.0;
+    if (!a.teacher_lse) {
+        double top = lg_wave_max(lp[0] > lp[1] || lp[0] != lp[0] ? lp[0] : lp[1]);
         if (top == -INFINITY) top = 0.0;
-        double norm = teacher_lse ? (double)*teacher_lse : 0.0;
-        if (!teacher_lse) {
-            for (int i = 0; i < k; ++i) sum += L.index[i] >= 0 ? exp(L.lp[i] - top) : 0.0;
-            norm = sum > 0.0 || sum != sum ? top + log(sum) : 0.0;
-        }
-        double P = 0.0, H = 0.0, count = 0.0, bad = 0.0;
-        for (int i = 0; i < k; ++i) {
-            const double lp = L.lp[i] - norm, p = L.index[i] >= 0 ? exp(lp) : 0.0;
-            L.lp[i] = lp;
-            L.p[i] = p;
-            P += p;
-            if (p != 0.0) H += p * lp;
-            count += L.index[i] >= 0;
-            bad += L.index[i] >= V;
-        }
-        L.sum[0] = P;
-        L.sum[1] = H;
-        L.sum[2] = count;
-        L.sum[3] = bad;
+        const double sum = wave_sum(exp(lp[0] - top) + exp(lp[1] - top));
+        norm = sum == 0.0 ? 0.0 : top + log(sum);
     }
-    __syncthreads();
-}
-
-// Sets the bits of the listed columns of [first, first + LG_SEGMENT) in bits
-__device__ void lg_mark(uint32_t* bits, const ListLds& L, int k, int first) {
-    __syncthreads();
-    for (int w = threadIdx.x; w < LG_SEGMENT / 32; w += LG_THREADS) bits[w] = 0;
-    __syncthreads();
-    if ((int)threadIdx.x < k) {
-        const int i = L.index[threadIdx.x] - first;
-        if (L.index[threadIdx.x] >= 0 && i >= 0 && i < LG_SEGMENT) atomicOr(bits + i / 32, 1u << (i % 32));
-    }
-    __syncthreads();
-}
-
-// stats of a row: shift m and factor f of the unlisted entries' gradient f 2^((x - m) c2); shift and log2 of the sum of all
-// entries.  Without a rest every entry counts as unlisted for m, and f = P / (S c).
-template <typename XT>
-__global__ __launch_bounds__(LG_THREADS) void distill_kernel(const XT* __restrict__ x, int64_t stride, int V,
-                                                             const float* __restrict__ top_logit, const int32_t* __restrict__ top_index,
-                                                             int k, const float* __restrict__ teacher_lse, float c,
-                                                             const float* __restrict__ weight, float* __restrict__ loss,
-                                                             float* __restrict__ stats) {
-    __shared__ float lds[LG_THREADS];
-    __shared__ ListLds L;
-    __shared__ uint32_t bits[LG_SEGMENT / 32];
-    const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x;
-    const XT* row = x + t * stride;
-    const float c2 = c * LG_LOG2E;
-    const bool rest = teacher_lse != nullptr;
-    if (weight && weight[t] == 0.f) {
-        if (tid == 0) loss[t] = 0.f;
-        return;
-    }
-    lg_load_list(L, row, V, top_logit + t * k, top_index + t * k, k, rest ? teacher_lse + t : nullptr, (double)c);
-    float m = -INFINITY;
-    for (int first = 0; first < V; first += LG_SEGMENT) {
-        if (rest) lg_mark(bits, L, k, first);
-        const int last = V - first < LG_SEGMENT ? V : first + LG_SEGMENT;
-        for (int i = first + tid; i < last; i += LG_THREADS)
-            if (!rest || !((bits[(i - first) / 32] >> ((i - first) % 32)) & 1u)) m = fmaxf(m, Elem<XT>::load(row + i));
-    }
-    m = lg_block_reduce(m, lg_max, lds);
-    float m_all = m;
-    if (m == -INFINITY) m = 0.f;
+    double P = 0.0, H = 0.0, U = 0.0;
+    const float m = lg_wave_max(lg_max2(s[0], s[1])), shift = lg_shift(m);
     float S = 0.f;
-    for (int first = 0; first < V; first += LG_SEGMENT) {
-        if (rest) lg_mark(bits, L, k, first);
-        const int last = V - first < LG_SEGMENT ? V : first + LG_SEGMENT;
-        for (int i = first + tid; i < last; i += LG_THREADS)
-            if (!rest || !((bits[(i - first) / 32] >> ((i - first) % 32)) & 1u)) S += lg_exp2((Elem<XT>::load(row + i) - m) * c2);
-    }
-    S = lg_block_reduce(S, lg_add, lds);
-    if (tid != 0) return;
-    double S_all = S;
-    int distinct = 0;
-    if (rest)
-        for (int i = 0; i < k; ++i) m_all = fmaxf(m_all, L.s[i]);
-    if (m_all == -INFINITY) m_all = 0.f;
-    if (rest) {
-        S_all = S == 0.f ? 0.0 : (double)S * exp2((double)((m - m_all) * c2));
-        for (int i = 0; i < k; ++i) {
-            bool twice = L.index[i] < 0;
-            for (int j = 0; j < i; ++j) twice |= L.index[j] == L.index[i];
-            if (twice) continue;
-            ++distinct;
-            S_all += exp2((double)((L.s[i] - m_all) * c2));
+    uint32_t distinct = 0;
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        p[u] = exp(lp[u] - norm);
+        P += p[u];
+        if (p[u] != 0.0) {
+            H += p[u] * (lp[u] - norm);
+            U += p[u] * ((double)(s[u] - shift) * a.c);
         }
+        L.p[lane + 64 * u] = (float)p[u];
+        bad |= j[u] >= a.V;
     }
-    const double l_all = S_all == 0.0 ? 0.0 : log(S_all);
-    double r = rest && distinct < V ? 1.0 - L.sum[0] : 0.0;
-    if (r < 0.0) r = 0.0;
-    double value = L.sum[1], factor = L.sum[0] / S_all;
-    for (int i = 0; i < k; ++i)
-        if (L.p[i] != 0.0) value -= L.p[i] * ((double)(L.s[i] - m_all) * c - l_all);
-    if (rest) {
-        const double lrest = log((double)S) + (double)((m - m_all) * c2) * M_LN2 - l_all;
-        if (r != 0.0) value += r * (log(r) - lrest);
-        factor = S == 0.f ? 0.0 : (exp(lrest) - r) / S;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // indices that stand more than once: every one of their entries gets the whole probability, one counts in S
+    float all[2] = {0.f, 0.f};
+    bool first[2] = {j[0] >= 0, j[1] >= 0};
+    for (int i = 0; i < a.k; ++i) {
+        const int at = L.index[i];
+        const float pi = L.p[i];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (at == j[u]) {
+                all[u] += pi;
+                if (i < lane + 64 * u) first[u] = false;
+            }
     }
-    factor /= c;
-    value /= (double)c * c;
-    double l2 = l_all * M_LOG2E;
-    if (S_all == 0.0) {  // nothing left
-        factor = 0.0;
-        l2 = -INFINITY;
-    }
-    if (L.sum[2] == 0.0) {
-        value = factor = 0.0;
-    } else if (L.sum[3] != 0.0) {
-        value = factor = l2 = NAN;
-    }
-    loss[t] = (float)value;
-    if (stats) {
-        stats[4 * t] = m;
-        stats[4 * t + 1] = (float)factor;
-        stats[4 * t + 2] = m_all;
-        stats[4 * t + 3] = (float)l2;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+        if (first[u]) {
+            S += lg_exp2((s[u] - shift) * c2);
+            ++distinct;
+        }
+    P = wave_sum(P);
+    H = wave_sum(H);
+    U = wave_sum(U);
+    S = lg_wave_sum(S);
+    distinct = wave_sum(distinct);
+    const bool any_bad = __ballot(bad) != 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // all reads of L.p are done
+    L.p[lane] = all[0];
+    L.p[lane + 64] = all[1];
+    if (lane == 0) {
+        L.P = P;
+        L.H = H;
+        L.U = U;
+        L.m = m;
+        L.S = S;
+        L.distinct = (int)distinct;
+        L.bad = any_bad;
     }
 }
 
-template <typename XT>
-__global__ __launch_bounds__(LG_THREADS) void distill_bwd_kernel(const XT* x, int64_t stride, int V, const float* __restrict__ top_logit,
-                                                                 const int32_t* __restrict__ top_index, int k,
-                                                                 const float* __restrict__ teacher_lse, float c,
-                                                                 const float* __restrict__ stats, const float* __restrict__ weight,
-                                                                 XT* dx, int64_t dstride) {
-    __shared__ ListLds L;
-    const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x;
-    const XT* row = x + t * stride;
-    XT* drow = dx + t * dstride;
+// What a row's gradient needs: unlisted (without a rest: all) entries f 2^((x - m) c2), listed ones P q - p over c.
+struct DistillStats {
+    float m, f, m_all, l2;  // l2: log2 of the sum of all entries relative to m_all; -inf: nothing left
+};
+
+// u: the unlisted entries' sums (without a rest: all entries').  loss != nullptr: also the loss, in 64 bits
+__device__ __forceinline__ DistillStats lg_distill_stats(const ListLds& L, Part u, float c, bool rest, int V, float* loss) {
     const float c2 = c * LG_LOG2E;
-    const float w = weight ? weight[t] : 1.f;
+    DistillStats d;
+    const float top = rest ? lg_max2(u.m, L.m) : u.m;
+    d.m = lg_shift(u.m);
+    d.m_all = lg_shift(top);
+    float S = u.S;  // of all
+    float other = 0.f;
+    if (rest) {
+        other = u.S * lg_exp2(lg_step(u.m, d.m_all, c2));
+        S = other + L.S * lg_exp2(lg_step(L.m, d.m_all, c2));
+    }
+    const bool none = S == 0.f, empty = L.distinct == 0;
+    double r = rest && L.distinct < V ? 1.0 - L.P : 0.0;
+    r = r < 0.0 ? 0.0 : r;  // NaN stays
+    d.l2 = log2f(S);
+    if (!rest) d.f = (float)L.P / S;
+    else d.f = u.S == 0.f && S == S ? 0.f : (other / S - (float)r) / u.S;
+    d.f /= c;
+    if (none || empty) d.f = 0.f;
+    if (loss) {
+        const double lS = none ? 0.0 : log((double)S);
+        double value = L.H;
+        if (L.P != 0.0) value -= L.U + L.P * ((double)(lg_shift(L.m) - d.m_all) * c - lS);
+        if (rest && r != 0.0) value += r * (log(r) - (log((double)u.S) + (double)(d.m - d.m_all) * c - lS));
+        value /= (double)c * c;
+        if (empty) value = 0.0;
+        else if (L.bad) value = NAN;
+        *loss = (float)value;
+    }
+    if (empty) d.l2 = -INFINITY;
+    else if (L.bad) d.f = d.l2 = NAN;
+    return d;
+}
+
+__device__ __forceinline__ void lg_write_distill(const DistillArgs& a, int64_t t, const DistillStats& d) {
+    if (!a.stats) return;
+    float* s = a.stats + 4 * t;
+    s[0] = d.m, s[1] = d.f, s[2] = d.m_all, s[3] = d.l2;
+}
+
+// gradient of listed entry i (its weight w, the factor 1 / c inside)
+__device__ __forceinline__ float lg_listed_gradient(const ListLds& L, const DistillStats& d, int i, float c, bool rest, float w) {
+    const float q = lg_exp2((L.s[i] - d.m_all) * (c * LG_LOG2E) - d.l2);
+    return d.l2 == -INFINITY ? 0.f : ((rest ? q : (float)L.P * q) - L.p[i]) * (w / c);
+}
+
+// One bit per entry of the chunk's vectors: listed or not
+template <typename XT, int NV>
+struct LgBits {
+    uint32_t* words;
+    __device__ __forceinline__ void zero(int per) {
+        for (int i = threadIdx.x; i < (per * LgVec<XT>::N + 31) / 32; i += blockDim.x) words[i] = 0;
+    }
+    __device__ __forceinline__ void set(const LgChunk<XT, NV>& chunk, const ListLds& L, int k) {
+        for (int i = threadIdx.x; i < k; i += blockDim.x) {
+            const int at = L.index[i] - chunk.head - chunk.first * LgVec<XT>::N;
+            if (L.index[i] >= chunk.head && at >= 0 && at < chunk.n * LgVec<XT>::N) atomicOr(words + at / 32, 1u << (at % 32));
+        }
+    }
+    // takes the listed entries out of the chunk
+    __device__ __forceinline__ void clear(LgChunk<XT, NV>& chunk, const ListLds& L, int k) const {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int j = i * (int)blockDim.x + (int)threadIdx.x;
+            if (j < chunk.n) {
+                const uint32_t bits = (words[j * LgVec<XT>::N / 32] >> (j * LgVec<XT>::N % 32)) & ((1u << LgVec<XT>::N) - 1u);
+                if (bits) LgVec<XT>::clear(chunk.w[i], bits);
+            }
+        }
+        if (chunk.edge_index >= 0)
+            for (int i = 0; i < k; ++i)
+                if (L.index[i] == chunk.edge_index) chunk.edge = -INFINITY;
+    }
+};
+
+// Sums of a chunk; or, of a row that is one chunk, the loss (and statistics), or loss and gradient
+enum DistillMode { LG_SUMS, LG_LOSS, LG_GRADIENT };
+template <typename XT, int NV, bool REST, DistillMode MODE>
+__global__ __launch_bounds__(LG_MAX_THREADS) void distill_kernel(DistillArgs a) {
+    __shared__ Part parts[16];
+    __shared__ ListLds L;
+    __shared__ uint32_t words[REST ? NV * LG_MAX_THREADS * LgVec<XT>::N / 32 : 1];
+    const int64_t t = a.row0 + blockIdx.x / (uint32_t)a.splits;
+    const int chunk_number = (int)(blockIdx.x % (uint32_t)a.splits);
+    const int tid = threadIdx.x, wave = tid >> 6, waves = blockDim.x >> 6;
+    const float c2 = a.c * LG_LOG2E;
+    XT* drow = static_cast<XT*>(a.dx) + t * a.dstride;
+    const float w = a.weight ? a.weight[t] : 1.f;
     if (w == 0.f) {
-        for (int i = tid; i < V; i += LG_THREADS) Elem<XT>::store(drow + i, 0.f);
+        if constexpr (MODE == LG_GRADIENT) lg_zero_row(drow, a.V, 0, 1);
+        if (MODE != LG_SUMS && tid == 0) a.loss[t] = 0.f;
         return;
     }
-    lg_load_list(L, row, V, top_logit + t * k, top_index + t * k, k, teacher_lse ? teacher_lse + t : nullptr, (double)c);
-    const float m = stats[4 * t], f = w * stats[4 * t + 1], m_all = stats[4 * t + 2], l2 = stats[4 * t + 3];
-    for (int i = tid; i < V; i += LG_THREADS) {
-        const float e = lg_exp2((Elem<XT>::load(row + i) - m) * c2);
-        Elem<XT>::store(drow + i, f == 0.f ? 0.f : f * e);
+    LgChunk<XT, NV> chunk;
+    chunk.load(static_cast<const XT*>(a.x) + t * a.stride, a.V, chunk_number, a.per);
+    LgBits<XT, NV> bits{words};
+    if constexpr (REST) bits.zero(a.per);
+    if constexpr (REST || MODE != LG_SUMS) {
+        if (wave == 0) lg_load_list<XT>(L, a, t);
+        __syncthreads();
     }
+    if constexpr (REST) {
+        bits.set(chunk, L, a.k);
+        __syncthreads();
+        bits.clear(chunk, L, a.k);
+    }
+    const float tm = chunk.max();
+    Part p = lg_wave_join<false>(chunk.template sums<false>(tm, c2), c2);
+    if ((tid & 63) == 0) parts[wave] = p;
     __syncthreads();
-    if (tid < k && L.index[tid] >= 0 && L.index[tid] < V) {
-        double p = 0.0;
-        for (int j = 0; j < k; ++j)
-            if (L.index[j] == L.index[tid]) p += L.p[j];
-        const double q = exp2((double)((L.s[tid] - m_all) * c2) - (double)l2);
-        const double P = teacher_lse ? 1.0 : L.sum[0];
-        Elem<XT>::store(drow + L.index[tid], l2 == -INFINITY ? 0.f : (float)((P * q - p) * w / c));
+    p = lg_parts_join<false>(parts, waves, c2);
+    if constexpr (MODE == LG_SUMS) {
+        if (tid == 0) a.parts[t * a.splits + chunk_number] = make_float4(p.m, p.S, 0.f, 0.f);
+    } else if constexpr (MODE == LG_LOSS) {
+        if (tid == 0) lg_write_distill(a, t, lg_distill_stats(L, p, a.c, REST, a.V, a.loss + t));
+    } else {
+        const DistillStats d = lg_distill_stats(L, p, a.c, REST, a.V, tid == 0 ? a.loss + t : nullptr);
+        const float f = w * d.f;
+        if (f == 0.f) chunk.store(drow, [&](float) { return 0.f; });
+        else chunk.store(drow, [&](float v) { return f * lg_exp2((v - d.m) * c2); });
+        __syncthreads();
+        if (tid < a.k && L.index[tid] >= 0 && L.index[tid] < a.V)
+            Elem<XT>::store(drow + L.index[tid], lg_listed_gradient(L, d, tid, a.c, REST, w));
+    }
+}
+
+// Joins the chunks of a row: one wave per row
+template <typename XT, bool REST>
+__global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a) {
+    __shared__ ListLds L;
+    const int64_t t = a.row0 + blockIdx.x;
+    const int lane = threadIdx.x;
+    if (a.weight && a.weight[t] == 0.f) {
+        if (lane == 0) a.loss[t] = 0.f;
+        return;
+    }
+    lg_load_list<XT>(L, a, t);
+    __syncthreads();
+    const float4 f = lane < a.splits ? a.parts[t * a.splits + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    const Part p = lg_wave_join<false>(Part{f.x, f.y, 0.f}, a.c * LG_LOG2E);
+    if (lane == 0) lg_write_distill(a, t, lg_distill_stats(L, p, a.c, REST, a.V, a.loss + t));
+}
+
+template <typename XT, int NV, bool REST>
+__global__ __launch_bounds__(256) void distill_bwd_kernel(DistillArgs a) {
+    __shared__ ListLds L;
+    const int64_t t = a.row0 + blockIdx.x / (uint32_t)a.splits;
+    const int chunk_number = (int)(blockIdx.x % (uint32_t)a.splits);
+    const int tid = threadIdx.x;
+    const float c2 = a.c * LG_LOG2E;
+    const XT* row = static_cast<const XT*>(a.x) + t * a.stride;
+    XT* drow = static_cast<XT*>(a.dx) + t * a.dstride;
+    const float w = a.weight ? a.weight[t] : 1.f;
+    if (w == 0.f) {
+        lg_zero_row(drow, a.V, chunk_number, a.splits);
+        return;
+    }
+    LgChunk<XT, NV> chunk;
+    chunk.load(row, a.V, chunk_number, a.per);
+    const float* s = a.stats + 4 * t;
+    const DistillStats d{s[0], s[1], s[2], s[3]};
+    if (tid < 64) lg_load_list<XT>(L, a, t);
+    __syncthreads();
+    const float f = w * d.f;
+    if (f == 0.f) chunk.store(drow, [&](float) { return 0.f; });
+    else chunk.store(drow, [&](float v) { return f * lg_exp2((v - d.m) * c2); });
+    __syncthreads();
+    // the listed entries of this chunk are written once more
+    if (tid < a.k && L.index[tid] >= 0 && L.index[tid] < a.V) {
+        const int vectors = (a.V - chunk.head) / LgVec<XT>::N;
+        const int v = L.index[tid] < chunk.head ? -1 : (L.index[tid] - chunk.head) / LgVec<XT>::N;
+        const bool edge = v < 0 || v >= vectors;
+        if (edge ? chunk_number == 0 : (v >= chunk.first && v < chunk.first + chunk.n))
+            Elem<XT>::store(drow + L.index[tid], lg_listed_gradient(L, d, tid, a.c, REST, w));
     }
 }
 
 }  // namespace bcq
+
+// ---- launches -------------------------------------------------------------------------------------------------------
+namespace {
+
+// How rows are cut: `splits` chunks of `per` vectors, `nv` vectors per thread, `threads` threads.
+struct Plan {
+    int splits, per, nv, threads;
+};
+
+int vector_entries(int dtype) { return dtype == BCQ_BF16 ? 8 : 4; }
+
+// For the forward passes.  Rows are cut where they do not fit a workgroup's registers, and where there are too few.
+Plan forward_plan(int64_t T, int64_t V, int dtype, int k) {
+    const int64_t vectors = (V + vector_entries(dtype) - 1) / vector_entries(dtype);
+    const int64_t least = (vectors + bcq::LG_MAX_NV * bcq::LG_MAX_THREADS - 1) / (bcq::LG_MAX_NV * bcq::LG_MAX_THREADS);
+    int64_t splits = (512 + T - 1) / (T > 0 ? T : 1);
+    const int64_t useful = (vectors + 511) / 512;
+    if (splits > useful) splits = useful;
+    if (splits > bcq::LG_MAX_SPLITS) splits = bcq::LG_MAX_SPLITS;
+    if (k > 0 && splits * k > bcq::LG_JOIN_CANDIDATES) splits = bcq::LG_JOIN_CANDIDATES / k;
+    if (splits < least) splits = least;
+    Plan p;
+    p.per = (int)((vectors + splits - 1) / splits);
+    p.splits = (int)((vectors + p.per - 1) / p.per);
+    p.nv = p.per <= 2 * bcq::LG_MAX_THREADS ? 2 : p.per <= 8 * bcq::LG_MAX_THREADS ? 8 : 16;
+    p.threads = ((p.per + p.nv - 1) / p.nv + 63) / 64 * 64;
+    if (p.threads < 256) p.threads = 256;
+    return p;
+}
+// For the gradients from saved statistics: nothing is joined, so chunks are small.
+constexpr int kBwdNv = 4;
+Plan backward_plan(int64_t V, int dtype) {
+    const int64_t vectors = (V + vector_entries(dtype) - 1) / vector_entries(dtype);
+    Plan p;
+    p.nv = kBwdNv;
+    p.threads = 256;
+    p.splits = (int)((vectors + kBwdNv * 256 - 1) / (kBwdNv * 256));
+    p.per = kBwdNv * 256;
+    return p;
+}
+
+// f(first row, rows) over slices of the rows that one launch can take: fewer than 2^31 threads
+template <typename F>
+void slices(int64_t T, int64_t threads_per_row, F f) {
+    const int64_t rows = (((int64_t)1 << 31) - 1) / threads_per_row;
+    for (int64_t t = 0; t < T; t += rows) f(t, (unsigned)(T - t < rows ? T - t : rows));
+}
+
+template <typename XT, int NV, bool ENT, bool TOP>
+void launch_logprobs_as(bcq::LogprobsArgs a, int64_t T, int threads, hipStream_t st) {
+    slices(T, (int64_t)a.splits * threads, [&](int64_t row0, unsigned rows) {
+        a.row0 = row0;
+        BCQ_LAUNCH((bcq::logprobs_kernel<XT, NV, ENT, TOP>), dim3(rows * a.splits), dim3(threads), 0, st, a);
+        if (a.splits > 1) BCQ_LAUNCH((bcq::logprobs_join_kernel<XT, ENT, TOP>), dim3(rows), dim3(TOP ? 256 : 64), 0, st, a);
+    });
+}
+template <typename XT, int NV>
+void launch_logprobs_nv(const bcq::LogprobsArgs& a, int64_t T, int threads, hipStream_t st) {
+    if (a.entropy) {
+        if (a.k) launch_logprobs_as<XT, NV, true, true>(a, T, threads, st);
+        else launch_logprobs_as<XT, NV, true, false>(a, T, threads, st);
+    } else if (a.k) launch_logprobs_as<XT, NV, false, true>(a, T, threads, st);
+    else launch_logprobs_as<XT, NV, false, false>(a, T, threads, st);
+}
+template <typename XT>
+hipError_t launch_logprobs(const bcq::LogprobsArgs& a, int64_t T, const Plan& p, hipStream_t st) {
+    if (p.nv == 2) launch_logprobs_nv<XT, 2>(a, T, p.threads, st);
+    else if (p.nv == 8) launch_logprobs_nv<XT, 8>(a, T, p.threads, st);
+    else launch_logprobs_nv<XT, 16>(a, T, p.threads, st);
+    return hipGetLastError();
+}
+template <typename XT>
+hipError_t launch_logprobs_bwd(bcq::LogprobsBwdArgs a, int64_t T, const Plan& p, hipStream_t st) {
+    slices(T, (int64_t)p.splits * p.threads, [&](int64_t row0, unsigned rows) {
+        a.row0 = row0;
+        if (a.dentropy) BCQ_LAUNCH((bcq::logprobs_bwd_kernel<XT, kBwdNv, true>), dim3(rows * p.splits), dim3(p.threads), 0, st, a);
+        else BCQ_LAUNCH((bcq::logprobs_bwd_kernel<XT, kBwdNv, false>), dim3(rows * p.splits), dim3(p.threads), 0, st, a);
+    });
+    return hipGetLastError();
+}
+
+template <typename XT, int NV, bool REST, bcq::DistillMode MODE>
+void launch_distill_as(bcq::DistillArgs a, int64_t T, int threads, hipStream_t st) {
+    slices(T, (int64_t)a.splits * threads, [&](int64_t row0, unsigned rows) {
+        a.row0 = row0;
+        BCQ_LAUNCH((bcq::distill_kernel<XT, NV, REST, MODE>), dim3(rows * a.splits), dim3(threads), 0, st, a);
+        if (MODE == bcq::LG_SUMS) BCQ_LAUNCH((bcq::distill_join_kernel<XT, REST>), dim3(rows), dim3(64), 0, st, a);
+    });
+}
+template <typename XT, bcq::DistillMode MODE>
+hipError_t launch_distill(const bcq::DistillArgs& a, int64_t T, const Plan& p, hipStream_t st) {
+    const bool rest = a.teacher_lse != nullptr;
+    if (p.nv == 2) rest ? launch_distill_as<XT, 2, true, MODE>(a, T, p.threads, st) : launch_distill_as<XT, 2, false, MODE>(a, T, p.threads, st);
+    else if (p.nv == 8) rest ? launch_distill_as<XT, 8, true, MODE>(a, T, p.threads, st) : launch_distill_as<XT, 8, false, MODE>(a, T, p.threads, st);
+    else rest ? launch_distill_as<XT, 16, true, MODE>(a, T, p.threads, st) : launch_distill_as<XT, 16, false, MODE>(a, T, p.threads, st);
+    return hipGetLastError();
+}
+template <typename XT>
+hipError_t launch_distill_bwd(bcq::DistillArgs a, int64_t T, const Plan& p, hipStream_t st) {
+    a.splits = p.splits;
+    a.per = p.per;
+    slices(T, (int64_t)p.splits * p.threads, [&](int64_t row0, unsigned rows) {
+        a.row0 = row0;
+        if (a.teacher_lse) BCQ_LAUNCH((bcq::distill_bwd_kernel<XT, kBwdNv, true>), dim3(rows * p.splits), dim3(p.threads), 0, st, a);
+        else BCQ_LAUNCH((bcq::distill_bwd_kernel<XT, kBwdNv, false>), dim3(rows * p.splits), dim3(p.threads), 0, st, a);
+    });
+    return hipGetLastError();
+}
+
+}  // namespace
 
 // ---- C entry points -----------------------------------------------------------------------------------------------
 namespace {
@@ -339,7 +1019,21 @@ bool off(const void* p) { return (reinterpret_cast<uintptr_t>(p) & (N - 1)) != 0
 bool off_element(const void* p, int dtype) { return dtype == BCQ_BF16 ? off<2>(p) : off<4>(p); }
 bcq_status done(hipError_t e) { return e == hipSuccess ? BCQ_OK : BCQ_ERR_DEVICE; }
 
-size_t workspace_need(int op, int64_t T) { return op == BCQ_OP_DISTILL_FWD_BWD ? (size_t)T * 16 : 0; }
+// The partial sums of split rows (16 bytes a chunk), then their lists of alternatives, or the statistics between a loss
+// and its gradient (16 bytes a row).
+size_t workspace_need(int op, int64_t T, int64_t V, int k, int dtype) {
+    const Plan p = forward_plan(T, V, dtype, op == BCQ_OP_LOGPROBS_FWD ? k : 0);
+    if (p.splits == 1) return 0;
+    const size_t parts = (size_t)T * p.splits * 16;
+    if (op == BCQ_OP_LOGPROBS_FWD) return parts + (size_t)T * p.splits * k * 8;
+    return parts + (op == BCQ_OP_DISTILL_FWD_BWD ? (size_t)T * 16 : 0);
+}
+bcq_status check_workspace(const void* ws, size_t have, size_t need) {
+    if (need == 0) return BCQ_OK;
+    if (!ws) return BCQ_ERR_NULL;
+    if (bcq::host::misaligned(ws)) return BCQ_ERR_ALIGN;
+    return have < need ? BCQ_ERR_WORKSPACE : BCQ_OK;
+}
 
 }  // namespace
 
@@ -352,7 +1046,7 @@ bcq_status bcq_logits_workspace_bytes(int op, int64_t T, int64_t V, int k, int d
     if (s != BCQ_OK) return s;
     if (op != BCQ_OP_LOGPROBS_FWD && k < 1) return BCQ_ERR_SHAPE;
     if (!dtype_ok(dtype)) return BCQ_ERR_DTYPE;
-    *out = workspace_need(op, T);
+    *out = workspace_need(op, T, V, k, dtype);
     return BCQ_OK;
 }
 
@@ -368,20 +1062,17 @@ bcq_status bcq_logprobs_fwd(const void* logits, int dtype, int64_t T, int64_t V,
     if (off_element(logits, dtype) || off<8>(tokens) || off<4>(logp) || off<4>(entropy) || off<4>(lse) || off<4>(stats) ||
         off<4>(top_index) || off<4>(top_logit) || off<4>(top_logp))
         return BCQ_ERR_ALIGN;
-    (void)workspace;
-    (void)workspace_bytes;
+    if (!top_index && !top_logit && !top_logp) k = 0;
+    s = check_workspace(workspace, workspace_bytes, workspace_need(BCQ_OP_LOGPROBS_FWD, T, V, k, dtype));
+    if (s != BCQ_OK) return s;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    const float c = 1.0f / temperature;
-    if (!top_index && !top_logit && !top_logp) k = 0;
-    const bcq::LogprobsOut out{logp, entropy, lse, stats, top_logit, top_logp, top_index};
+    const Plan p = forward_plan(T, V, dtype, k);
+    float4* parts = static_cast<float4*>(workspace);
+    const bcq::LogprobsArgs a{logits, row_stride, tokens, 1.0f / temperature, (int)V, k, p.splits, p.per, 0, logp, entropy, lse, stats,
+                              top_logit, top_logp, top_index, parts, reinterpret_cast<uint64_t*>(parts + T * p.splits)};
     hipStream_t st = (hipStream_t)stream;
-    const dim3 grid((unsigned)T), block(bcq::LG_THREADS);
-    if (dtype == BCQ_BF16)
-        BCQ_LAUNCH(bcq::logprobs_kernel<bcq::bf16_t>, grid, block, 0, st, (const bcq::bf16_t*)logits, row_stride, (int)V, tokens, c, k, out);
-    else
-        BCQ_LAUNCH(bcq::logprobs_kernel<float>, grid, block, 0, st, (const float*)logits, row_stride, (int)V, tokens, c, k, out);
-    return done(hipGetLastError());
+    return done(dtype == BCQ_BF16 ? launch_logprobs<bcq::bf16_t>(a, T, p, st) : launch_logprobs<float>(a, T, p, st));
 }
 
 bcq_status bcq_logprobs_bwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride, const int64_t* tokens,
@@ -400,16 +1091,11 @@ bcq_status bcq_logprobs_bwd(const void* logits, int dtype, int64_t T, int64_t V,
         return BCQ_ERR_ALIGN;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    const float c = 1.0f / temperature;
+    const Plan p = backward_plan(V, dtype);
+    const bcq::LogprobsBwdArgs a{logits, row_stride, tokens, stats, dlogp, entropy, dentropy, 1.0f / temperature, (int)V, p.splits,
+                                 p.per, 0, dlogits, grad_stride};
     hipStream_t st = (hipStream_t)stream;
-    const dim3 grid((unsigned)T), block(bcq::LG_THREADS);
-    if (dtype == BCQ_BF16)
-        BCQ_LAUNCH(bcq::logprobs_bwd_kernel<bcq::bf16_t>, grid, block, 0, st, (const bcq::bf16_t*)logits, row_stride, (int)V, tokens, c,
-                   stats, dlogp, entropy, dentropy, (bcq::bf16_t*)dlogits, grad_stride);
-    else
-        BCQ_LAUNCH(bcq::logprobs_bwd_kernel<float>, grid, block, 0, st, (const float*)logits, row_stride, (int)V, tokens, c, stats,
-                   dlogp, entropy, dentropy, (float*)dlogits, grad_stride);
-    return done(hipGetLastError());
+    return done(dtype == BCQ_BF16 ? launch_logprobs_bwd<bcq::bf16_t>(a, T, p, st) : launch_logprobs_bwd<float>(a, T, p, st));
 }
 
 }  // extern "C"
@@ -437,28 +1123,27 @@ bool distill_misaligned(const DistillCall& a) {
     return off_element(a.logits, a.dtype) || off<4>(a.top_logit) || off<4>(a.top_index) || off<4>(a.teacher_lse);
 }
 
-hipError_t run_distill_fwd(const DistillCall& a, const float* weight, float* loss, float* stats, hipStream_t st) {
-    const dim3 grid((unsigned)a.T), block(bcq::LG_THREADS);
-    const float c = 1.0f / a.temperature;
-    if (a.dtype == BCQ_BF16)
-        BCQ_LAUNCH(bcq::distill_kernel<bcq::bf16_t>, grid, block, 0, st, (const bcq::bf16_t*)a.logits, a.row_stride, (int)a.V, a.top_logit,
-                   a.top_index, a.k, a.teacher_lse, c, weight, loss, stats);
-    else
-        BCQ_LAUNCH(bcq::distill_kernel<float>, grid, block, 0, st, (const float*)a.logits, a.row_stride, (int)a.V, a.top_logit,
-                   a.top_index, a.k, a.teacher_lse, c, weight, loss, stats);
-    return hipGetLastError();
+bcq::DistillArgs distill_args(const DistillCall& a) {
+    bcq::DistillArgs d{};
+    d.x = a.logits;
+    d.stride = a.row_stride;
+    d.top_logit = a.top_logit;
+    d.top_index = a.top_index;
+    d.teacher_lse = a.teacher_lse;
+    d.c = 1.0f / a.temperature;
+    d.V = (int)a.V;
+    d.k = a.k;
+    return d;
 }
-hipError_t run_distill_bwd(const DistillCall& a, const float* stats, const float* weight, void* dlogits, int64_t grad_stride,
-                           hipStream_t st) {
-    const dim3 grid((unsigned)a.T), block(bcq::LG_THREADS);
-    const float c = 1.0f / a.temperature;
-    if (a.dtype == BCQ_BF16)
-        BCQ_LAUNCH(bcq::distill_bwd_kernel<bcq::bf16_t>, grid, block, 0, st, (const bcq::bf16_t*)a.logits, a.row_stride, (int)a.V,
-                   a.top_logit, a.top_index, a.k, a.teacher_lse, c, stats, weight, (bcq::bf16_t*)dlogits, grad_stride);
-    else
-        BCQ_LAUNCH(bcq::distill_bwd_kernel<float>, grid, block, 0, st, (const float*)a.logits, a.row_stride, (int)a.V, a.top_logit,
-                   a.top_index, a.k, a.teacher_lse, c, stats, weight, (float*)dlogits, grad_stride);
-    return hipGetLastError();
+template <bcq::DistillMode MODE>
+hipError_t run_distill(bcq::DistillArgs d, const DistillCall& a, const Plan& p, hipStream_t st) {
+    d.splits = p.splits;
+    d.per = p.per;
+    return a.dtype == BCQ_BF16 ? launch_distill<bcq::bf16_t, MODE>(d, a.T, p, st) : launch_distill<float, MODE>(d, a.T, p, st);
+}
+hipError_t run_distill_bwd(const bcq::DistillArgs& d, const DistillCall& a, hipStream_t st) {
+    const Plan p = backward_plan(a.V, a.dtype);
+    return a.dtype == BCQ_BF16 ? launch_distill_bwd<bcq::bf16_t>(d, a.T, p, st) : launch_distill_bwd<float>(d, a.T, p, st);
 }
 
 }  // namespace
@@ -474,11 +1159,17 @@ bcq_status bcq_distill_fwd(const void* logits, int dtype, int64_t T, int64_t V, 
     if (s != BCQ_OK) return s;
     if (!dtype_ok(dtype)) return BCQ_ERR_DTYPE;
     if (distill_misaligned(a) || off<4>(loss) || off<4>(stats)) return BCQ_ERR_ALIGN;
-    (void)workspace;
-    (void)workspace_bytes;
+    const bcq_status w = check_workspace(workspace, workspace_bytes, workspace_need(BCQ_OP_DISTILL_FWD, T, V, k, dtype));
+    if (w != BCQ_OK) return w;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    return done(run_distill_fwd(a, nullptr, loss, stats, (hipStream_t)stream));
+    const Plan p = forward_plan(T, V, dtype, 0);
+    bcq::DistillArgs d = distill_args(a);
+    d.loss = loss;
+    d.stats = stats;
+    d.parts = static_cast<float4*>(workspace);
+    hipStream_t st = (hipStream_t)stream;
+    return done(p.splits == 1 ? run_distill<bcq::LG_LOSS>(d, a, p, st) : run_distill<bcq::LG_SUMS>(d, a, p, st));
 }
 
 bcq_status bcq_distill_bwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride, const float* top_logit,
@@ -494,7 +1185,12 @@ bcq_status bcq_distill_bwd(const void* logits, int dtype, int64_t T, int64_t V, 
     if (distill_misaligned(a) || off_element(dlogits, dtype) || off<4>(stats) || off<4>(dloss)) return BCQ_ERR_ALIGN;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    return done(run_distill_bwd(a, stats, dloss, dlogits, grad_stride, (hipStream_t)stream));
+    bcq::DistillArgs d = distill_args(a);
+    d.weight = dloss;
+    d.stats = const_cast<float*>(stats);
+    d.dx = dlogits;
+    d.dstride = grad_stride;
+    return done(run_distill_bwd(d, a, (hipStream_t)stream));
 }
 
 bcq_status bcq_distill_fwd_bwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride,
@@ -509,16 +1205,22 @@ bcq_status bcq_distill_fwd_bwd(const void* logits, int dtype, int64_t T, int64_t
     if (logits == dlogits && row_stride != grad_stride) return BCQ_ERR_SHAPE;
     if (!dtype_ok(dtype)) return BCQ_ERR_DTYPE;
     if (distill_misaligned(a) || off_element(dlogits, dtype) || off<4>(weight) || off<4>(loss)) return BCQ_ERR_ALIGN;
-    const size_t need = workspace_need(BCQ_OP_DISTILL_FWD_BWD, T);
-    if (need && !workspace) return BCQ_ERR_NULL;
-    if (need && bcq::host::misaligned(workspace)) return BCQ_ERR_ALIGN;
-    if (workspace_bytes < need) return BCQ_ERR_WORKSPACE;
+    s = check_workspace(workspace, workspace_bytes, workspace_need(BCQ_OP_DISTILL_FWD_BWD, T, V, k, dtype));
+    if (s != BCQ_OK) return s;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    float* stats = static_cast<float*>(workspace);
-    const hipError_t e = run_distill_fwd(a, weight, loss, stats, (hipStream_t)stream);
-    if (e != hipSuccess) return BCQ_ERR_DEVICE;
-    return done(run_distill_bwd(a, stats, weight, dlogits, grad_stride, (hipStream_t)stream));
+    const Plan p = forward_plan(T, V, dtype, 0);
+    bcq::DistillArgs d = distill_args(a);
+    d.weight = weight;
+    d.loss = loss;
+    d.dx = dlogits;
+    d.dstride = grad_stride;
+    hipStream_t st = (hipStream_t)stream;
+    if (p.splits == 1) return done(run_distill<bcq::LG_GRADIENT>(d, a, p, st));
+    d.parts = static_cast<float4*>(workspace);
+    d.stats = reinterpret_cast<float*>(d.parts + T * p.splits);
+    const hipError_t e = run_distill<bcq::LG_SUMS>(d, a, p, st);
+    return e == hipSuccess ? done(run_distill_bwd(d, a, st)) : BCQ_ERR_DEVICE;
 }
 
 }  // extern "C"
