@@ -154,17 +154,29 @@ struct LgChunk {
     float edge;      // an entry before or behind the row's vectors (-inf for none), of the first threads of the first chunk
     int edge_index;  // its column, -1 for none
     int head;        // entries before the row's first whole vector
+    int vectors;     // of the row
     int first, n;    // the chunk's vectors
+    int threads;     // that hold them
 
-    // chunk number `chunk` of `per` vectors of the row
-    __device__ __forceinline__ void load(const XT* row, int V, int chunk, int per) {
-        const int tid = threadIdx.x, threads = blockDim.x;
+    // The geometry of chunk number `chunk` of `per` vectors of the row
+    __device__ __forceinline__ void place(const XT* row, int V, int chunk, int per) {
         const int skip = (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(XT);
         head = skip < V ? skip : V;
-        const int vectors = (V - head) / Vec::N;
+        vectors = (V - head) / Vec::N;
         first = chunk * per;
         const int left = vectors - first;
         n = left < per ? (left > 0 ? left : 0) : per;
+        edge_index = -1;
+        if (chunk == 0) {
+            const int tail = head + vectors * Vec::N, tid = threadIdx.x;
+            const int i = tid < head ? tid : tail + (tid - head);
+            if (i < V) edge_index = i;
+        }
+    }
+    // and its entries, dealt to the first `threads_` threads
+    __device__ __forceinline__ void load(const XT* row, int threads_) {
+        const int tid = threadIdx.x;
+        threads = threads_;
         if (n > 0) {
             const char* base = reinterpret_cast<const char*>(row + head) + (int64_t)first * 16;
 #pragma unroll
@@ -174,21 +186,32 @@ struct LgChunk {
                 w[i][0] = q.x, w[i][1] = q.y, w[i][2] = q.z, w[i][3] = q.w;
             }
         }
-        edge_index = -1;
-        if (chunk == 0) {
-            const int tail = head + vectors * Vec::N;
-            const int i = tid < head ? tid : tail + (tid - head);
-            if (i < V) edge_index = i;
-        }
         edge = edge_index >= 0 ? Elem<XT>::load(row + edge_index) : -INFINITY;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if ((i + 1) * threads > n && i * threads + tid >= n) w[i][0] = w[i][1] = w[i][2] = w[i][3] = Vec::NONE;
     }
-    __device__ __forceinline__ int column(int i, int e) const {
-        return head + (first + i * (int)blockDim.x + (int)threadIdx.x) * Vec::N + e;
+    // The entries are not used any more on this path: their registers are free before.
+    __device__ __forceinline__ void forget() {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) asm volatile("" : "=v"(w[i][u]));
     }
-    __device__ __forceinline__ bool any(int i) const { return i * (int)blockDim.x < n; }  // the same in all lanes
+    // A number for every column of the chunk, -1 for others: the row's unaligned begin, the vectors (a whole number of
+    // vectors from 0), the row's unaligned end
+    __device__ __forceinline__ int spot(int column, int V) const {
+        if (column < 0 || column >= V) return -1;
+        const int at = column - head;
+        if (at < 0) return first == 0 ? at + Vec::N : -1;
+        if (at >= vectors * Vec::N) return first == 0 ? at - (vectors - n - 1) * Vec::N : -1;
+        return at >= first * Vec::N && at < (first + n) * Vec::N ? at - (first - 1) * Vec::N : -1;
+    }
+    // the place of the thread's vector i in the chunk; `has`: there is one
+    __device__ __forceinline__ int place_of(int i) const { return i * threads + (int)threadIdx.x; }
+    __device__ __forceinline__ bool has(int i) const { return place_of(i) < n && (int)threadIdx.x < threads; }
+    __device__ __forceinline__ int column(int i, int e) const { return head + (first + place_of(i)) * Vec::N + e; }
+    __device__ __forceinline__ bool any(int i) const { return i * threads < n; }  // the same in all lanes
 
     __device__ __forceinline__ float max() const {
         float m = edge;
@@ -207,6 +230,14 @@ struct LgChunk {
             if (any(i))
 #pragma unroll
                 for (int u = 0; u < 4; ++u) Vec::quiet(w[i][u]);
+    }
+    // The values of bf16 words are taken apart anew in every pass: kept from one pass to the next they would need twice
+    // the registers of the words, and one workgroup less would fit a compute unit.
+    __device__ __forceinline__ void reread() {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) asm volatile("" : "+v"(w[i][u]));
     }
     // sums relative to the thread's own maximum
     template <bool ENT>
@@ -237,7 +268,7 @@ struct LgChunk {
         if (edge_index >= 0 && keep(edge)) f(edge, edge_index);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (any(i) && i * (int)blockDim.x + (int)threadIdx.x < n) {
+            if (any(i) && has(i)) {
                 float m = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < Vec::N; e += 2) m = lg_max3(m, Vec::get(w[i], e), Vec::get(w[i], e + 1));
@@ -249,16 +280,17 @@ struct LgChunk {
                     }
             }
     }
-    // number of entries of this thread for which keep(value, column)
-    template <typename K>
-    __device__ __forceinline__ uint32_t count(K keep) const {
-        uint32_t c = edge_index >= 0 && keep(edge, edge_index);
+    // f(value, column) of the thread's entries, read from memory once more
+    template <typename F>
+    __device__ __forceinline__ void scan(const XT* row, F f) const {
+        if (edge_index >= 0) f(Elem<XT>::load(row + edge_index), edge_index);
+        const uint4* base = reinterpret_cast<const uint4*>(row + head) + first;
+        for (int j = threadIdx.x; j < n; j += blockDim.x) {
+            const uint4 q = base[j];
+            const uint32_t v[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (any(i) && i * (int)blockDim.x + (int)threadIdx.x < n)
-#pragma unroll
-                for (int e = 0; e < Vec::N; ++e) c += keep(Vec::get(w[i], e), column(i, e)) ? 1u : 0u;
-        return c;
+            for (int e = 0; e < Vec::N; ++e) f(Vec::get(v, e), head + (first + j) * Vec::N + e);
+        }
     }
     // row[column] = f(value) for every entry of the chunk
     template <typename F>
@@ -274,9 +306,8 @@ struct LgChunk {
                 uint32_t q[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) q[u] = Vec::pack(v, u);
-                const int j = i * (int)blockDim.x + (int)threadIdx.x;
                 // the gradient's rows may be aligned otherwise than the logits'
-                if (j < n) __builtin_memcpy(base + (uint32_t)j * 16u, q, 16);
+                if (has(i)) __builtin_memcpy(base + (uint32_t)place_of(i) * 16u, q, 16);
             }
     }
 };
@@ -336,57 +367,81 @@ __device__ __forceinline__ void lg_write_top(const LogprobsArgs& a, int64_t t, i
     if (a.top_logp) a.top_logp[at] = p.S == 0.f ? -INFINITY : (v - lg_shift(p.m)) * a.c - l2 * LG_LN2;
 }
 
-// put(rank, entry) for the k first of the n entries in `list` by rank, and entry 0 for ranks beyond n
+// put(rank, entry) for the k first of the n entries in `list` by rank, and entry 0 for ranks beyond n.  Eight lanes share a
+// candidate, each comparing it with an eighth of the others.
 template <typename F>
 __device__ __forceinline__ void lg_rank(const uint64_t* list, int n, int k, F put) {
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const uint64_t mine = list[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
-        if (rank < k) put(rank, mine);
+    const int part = threadIdx.x & 7, groups = blockDim.x >> 3;
+    for (int first = 0; first < n; first += groups) {
+        const int i = first + (int)(threadIdx.x >> 3);
+        const uint64_t mine = list[i < n ? i : 0];
+        uint32_t rank = 0;
+#pragma unroll 4
+        for (int j = part; j < n; j += 8) rank += list[j] > mine ? 1u : 0u;
+        rank += dpp_move<DPP_XOR1>(rank);
+        rank += dpp_move<DPP_XOR2>(rank);
+        rank += dpp_move<DPP_HALF_MIRROR>(rank);
+        if (part == 0 && i < n && (int)rank < k) put((int)rank, mine);
     }
     for (int r = n + (int)threadIdx.x; r < k; r += blockDim.x) put(r, (uint64_t)0);
 }
 
 struct TopLds {
-    float max[LG_MAX_THREADS];  // of every thread
+    alignas(16) float max[LG_MAX_THREADS];  // of every thread
     uint64_t list[LG_CANDIDATES];
     uint32_t counts[2][16];
     int n;
 };
 
-// The candidates for a chunk's k best in lds.list, and their number.  At least k threads have a maximum that reaches the k-th
-// largest of the threads' maxima, so that value is a lower bound of the k-th entry, and few entries exceed it: of n random
-// entries over 832 threads about k + k^2 / 1700.  The bound only has to be low enough, so its search stops early.
+// The candidates for a chunk's k best in lds.list, and their number.  The threads are cut into 64 R groups, R the least power
+// of two with 32 R >= k.  At least k groups have a maximum that reaches the k-th largest of the groups' maxima, so that value
+// is a lower bound of the k-th entry, and few entries exceed it: with entries in random order -64 R ln(1 - k / (64 R)), 24 for
+// the 20 best, 74 for 64.  The bound only has to be low enough, so its search by halving stops early.
 // Called by all threads after lds.max is written and a barrier; lds.n is 0.
 template <typename XT, int NV>
-__device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>& chunk, float tm, int k) {
+__device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>& chunk, const XT* row, int V, float tm, int k) {
     const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-    uint32_t key[16];
-    float most = -INFINITY, least = -INFINITY;  // of the maxima; the least one's negative
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        key[v] = 0;
-        if (v < waves) {
-            const float x = lds.max[v * 64 + lane];
-            key[v] = lg_key(x);
-            most = lg_max2(most, x);
-            least = lg_max2(least, -x);
+    float group[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    for (int i = lane; i < (int)blockDim.x / 4; i += 64) {
+        const float4 q = reinterpret_cast<const float4*>(lds.max)[i];
+        group[0] = lg_max2(group[0], q.x);
+        group[1] = lg_max2(group[1], q.y);
+        group[2] = lg_max2(group[2], q.z);
+        group[3] = lg_max2(group[3], q.w);
+    }
+    if (k <= 64) {
+        group[0] = lg_max2(group[0], group[2]);
+        group[1] = lg_max2(group[1], group[3]);
+        group[2] = group[3] = -INFINITY;
+        if (k <= 32) {
+            group[0] = lg_max2(group[0], group[1]);
+            group[1] = -INFINITY;
         }
     }
-    uint32_t low = lg_key(-INFINITY);
-    uint32_t high = lg_key(lg_wave_max(most)) + 1;  // no entry reaches it
-    if ((int)blockDim.x >= k) {
-        low = lg_key(-lg_wave_max(least));
-        uint32_t reach = blockDim.x, above = high;
-        while (above - low > 1 && (int)reach > k + 8 + k / 4) {
-            const uint32_t mid = low + (above - low) / 2;
-            uint32_t c = 0;
+    uint32_t key[4], low = lg_key(-INFINITY);
+    float most = -INFINITY;
 #pragma unroll
-            for (int v = 0; v < 16; ++v)
-                if (v < waves) c += (uint32_t)__popcll(__ballot(key[v] >= mid));
-            if ((int)c >= k) low = mid, reach = c;
-            else above = mid;
+    for (int u = 0; u < 4; ++u) {
+        most = lg_max2(most, group[u]);
+        key[u] = lg_key(group[u]);
+    }
+    uint32_t high = lg_key(lg_wave_max(most)) + 1;  // no entry reaches it
+    auto reached = [&](uint32_t at) {
+        uint32_t c = (uint32_t)__popcll(__ballot(key[0] >= at));
+        if (k > 32) c += (uint32_t)__popcll(__ballot(key[1] >= at));
+        if (k > 64) c += (uint32_t)(__popcll(__ballot(key[2] >= at)) + __popcll(__ballot(key[3] >= at)));
+        return (int)c;
+    };
+    {
+        int reach = 256;
+        uint32_t over = high, step = 1u << 21;  // the first steps down from the maximum: a quarter of it each, doubled
+        while (over - low > 1 && reach > k + 8 + k / 4) {
+            const uint32_t half = low + (over - low) / 2, down = over - low > step ? over - step : half;
+            const uint32_t mid = reach == 256 && down > half ? down : half;
+            const int c = reached(mid);
+            if (step < 1u << 30) step *= 2;
+            if (c >= k) low = mid, reach = c;
+            else over = mid;
         }
     }
     const float bound = lg_unkey(low);
@@ -400,52 +455,68 @@ __device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>&
     int n = lds.n;
     if (n <= LG_CANDIDATES) return n;
 
-    // Too many: many equal entries (masked rows), or rows whose large entries meet in few threads.  Exact search for the
-    // k-th value by halving, counting entries in registers, then for the column up to which entries of that value count.
+    // Too many: equal entries in great number, as masks leave them, or large entries that meet in few threads.
     __syncthreads();
-    uint32_t greater = 0;  // entries that reach `high`
     int turn = 0;
-    auto total = [&](uint32_t c) {
+    auto above = [&](float at) {  // number of entries above a value
+        uint32_t c = 0;
+        chunk.scan(row, [&](float x, int) { c += x > at ? 1u : 0u; });
         c = wave_sum(c);
-        if (lane == 0) lds.counts[turn & 1][threadIdx.x >> 6] = c;
+        turn ^= 1;  // the counts of the last call may still be read
+        if (lane == 0) lds.counts[turn][threadIdx.x >> 6] = c;
         __syncthreads();
-        uint32_t s = 0;
-        for (int v = 0; v < waves; ++v) s += lds.counts[turn & 1][v];
-        ++turn;
-        return s;
+        int total = 0;
+        for (int v = 0; v < waves; ++v) total += (int)lds.counts[turn][v];
+        return total;
     };
-    uint32_t reach = (uint32_t)n;  // entries that reach `low`
-    while (high - low > 1) {
-        const uint32_t mid = low + (high - low) / 2;
-        const float at = lg_unkey(mid);
-        const uint32_t c = total(chunk.count([&](float x, int) { return x >= at; }));
-        if ((int)c >= k) low = mid, reach = c;
-        else high = mid, greater = c;
+    // where the entries above the bound are still too many, it is moved to the k-th value by halving
+    int greater = above(lg_unkey(low));
+    if (greater > LG_CANDIDATES) {
+        while (high - low > 1) {  // k or more exceed `low`, fewer than k exceed `high`
+            const uint32_t mid = low + (high - low) / 2;
+            if (above(lg_unkey(mid)) >= k) low = mid;
+            else high = mid;
+        }
+        low = high;
+        greater = above(lg_unkey(low));
     }
     const float value = lg_unkey(low);
-    int last = INT_MAX;
-    if (reach > LG_CANDIDATES) {
-        int below = -1;  // greater + entries of the value up to `below` < k; up to `last` >= k
-        last = BCQ_LOGITS_MAX_V;
-        while (last - below > 1) {
-            const int mid = below + (last - below) / 2;
-            const uint32_t c = total(chunk.count([&](float x, int index) { return x == value && index <= mid; }));
-            if ((int)(greater + c) >= k) last = mid;
-            else below = mid;
-        }
-    }
     if (threadIdx.x == 0) lds.n = 0;
     __syncthreads();
-    chunk.each([&](float x) { return x >= value; },
-               [&](float x, int index) {
-                   if (x > value || index <= last) {
-                       const int at = atomicAdd(&lds.n, 1);
-                       if (at < LG_CANDIDATES) lds.list[at] = lg_entry(x, index);
-                   }
-               });
+    chunk.scan(row, [&](float x, int index) {
+        if (x > value) lds.list[atomicAdd(&lds.n, 1)] = lg_entry(x, index);
+    });
     __syncthreads();
-    n = lds.n;
-    return n < LG_CANDIDATES ? n : LG_CANDIDATES;
+    n = greater;
+    if (n >= k) return n;
+    // the others equal the bound: the first of them by column, which the first wave looks for in order
+    if (threadIdx.x < 64) {
+        const int begin = chunk.first == 0 ? 0 : chunk.head + chunk.first * LgVec<XT>::N;
+        const int end = chunk.head + (chunk.first + chunk.n) * LgVec<XT>::N;
+        const int tail = chunk.head + (V - chunk.head) / LgVec<XT>::N * LgVec<XT>::N;
+        int at = n;
+        for (int part = 0; part < 2; ++part) {
+            const int from = part ? (end > tail ? end : tail) : begin, to = part ? (chunk.first == 0 ? V : 0) : end;
+            for (int i = from; i < to && at < k; i += 256) {
+                float x[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int j = i + u * 64 + lane;
+                    x[u] = j < to ? Elem<XT>::load(row + j) : NAN;
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint64_t equal = __ballot(x[u] == value);
+                    const int mine = at + __popcll(equal & (((uint64_t)1 << lane) - 1));
+                    if (x[u] == value && mine < k) lds.list[mine] = lg_entry(value, i + u * 64 + lane);
+                    at += __popcll(equal);
+                }
+            }
+        }
+        if (lane == 0) lds.n = at < k ? at : k;
+    }
+    __syncthreads();
+    return lds.n;
 }
 
 template <typename XT, int NV, bool ENT, bool TOP>
@@ -464,10 +535,14 @@ __global__ __launch_bounds__(LG_MAX_THREADS) void logprobs_kernel(LogprobsArgs a
         }
         return;
     }
+    const XT* row = static_cast<const XT*>(a.x) + t * a.stride;
     LgChunk<XT, NV> chunk;
-    chunk.load(static_cast<const XT*>(a.x) + t * a.stride, a.V, chunk_number, a.per);
+    chunk.place(row, a.V, chunk_number, a.per);
+    chunk.load(row, blockDim.x);
     float tm = chunk.max();
+    chunk.reread();
     Part p = lg_wave_join<ENT>(chunk.template sums<ENT>(tm, c2), c2);
+    chunk.reread();
     if ((tid & 63) == 0) parts[wave] = p;
     if constexpr (TOP) {
         top.max[tid] = tm;
@@ -488,7 +563,7 @@ __global__ __launch_bounds__(LG_MAX_THREADS) void logprobs_kernel(LogprobsArgs a
             top.max[tid] = tm;
             __syncthreads();
         }
-        const int n = lg_candidates<XT, NV>(top, chunk, tm, a.k);
+        const int n = lg_candidates<XT, NV>(top, chunk, row, a.V, tm, a.k);
         if (whole) lg_rank(top.list, n, a.k, [&](int rank, uint64_t entry) { lg_write_top(a, t, rank, entry, p, l2); });
         else {
             uint64_t* list = a.lists + (t * a.splits + chunk_number) * a.k;
@@ -562,15 +637,14 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(LogprobsBwdArgs a) {
     }
     if (token >= V) g = NAN;
     LgChunk<XT, NV> chunk;
-    chunk.load(row, V, chunk_number, a.per);
+    chunk.place(row, V, chunk_number, a.per);
+    chunk.load(row, blockDim.x);
     const float c2 = c * LG_LOG2E;
     // the token's entry is written once more, by the workgroup that has its chunk
     int mine = -1;
     float at = 0.f;
     if (threadIdx.x == 0 && token >= 0 && token < V) {
-        const int v = (int)token < chunk.head ? -1 : ((int)token - chunk.head) / LgVec<XT>::N;
-        const bool edge = v < 0 || v >= (V - chunk.head) / LgVec<XT>::N;
-        if (edge ? chunk_number == 0 : (v >= chunk.first && v < chunk.first + chunk.n)) {
+        if (chunk.spot((int)token, V) >= 0) {
             mine = (int)token;
             at = Elem<XT>::load(row + token);
         }
@@ -610,23 +684,18 @@ struct ListLds {
     int index[BCQ_LOGITS_MAX_K];
     float s[BCQ_LOGITS_MAX_K];
     float p[BCQ_LOGITS_MAX_K];  // the teacher's probability of the entry's index (of all entries with this index)
-    double P, H, U;             // sum of p; sum of p ln p; sum of p (s - m) c
+    uint16_t slot[2048];        // entries by their index' lowest bits
+    double P, H, U, norm;       // sum of p; of p ln p; of p (s - m) c; ln p = z c - norm
     float m, S;                 // the listed entries' maximum and sum, every index once
     int distinct, bad;          // listed indices; whether one is out of range
 };
 
-__device__ __forceinline__ double lg_wave_max(double v) {
-    for (int s = 1; s < 64; s *= 2) {
-        const double o = __shfl_xor(v, s);
-        v = o > v || o != o ? o : v;
-    }
-    return v;
-}
+__device__ __forceinline__ void lg_wave_sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// By the first wave alone, two entries a lane; the caller's barrier follows.
-template <typename XT>
+// By one wave alone, two entries a lane; the caller's barrier follows.  REST: the listed entries' sum is needed.
+template <typename XT, bool REST>
 __device__ __forceinline__ void lg_load_list(ListLds& L, const DistillArgs& a, int64_t t) {
-    const int lane = threadIdx.x;
+    const int lane = threadIdx.x & 63;
     const XT* row = static_cast<const XT*>(a.x) + t * a.stride;
     const float* z = a.top_logit + t * a.k;
     const int32_t* index = a.top_index + t * a.k;
@@ -638,23 +707,43 @@ __device__ __forceinline__ void lg_load_list(ListLds& L, const DistillArgs& a, i
     for (int u = 0; u < 2; ++u) {
         const int i = lane + 64 * u;
         j[u] = i < a.k ? index[i] : -1;
-        lp[u] = j[u] >= 0 ? (double)z[i] * a.c : -INFINITY;
-        s[u] = j[u] >= 0 && j[u] < a.V ? Elem<XT>::load(row + j[u]) : -INFINITY;
+        lp[u] = i < a.k ? (double)z[i] * a.c : -INFINITY;
         L.index[i] = j[u];
-        L.s[i] = s[u];
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    double norm = a.teacher_lse ? (double)a.teacher_lse[t] : 0.0;
-    if (!a.teacher_lse) {
-        double top = lg_wave_max(lp[0] > lp[1] || lp[0] != lp[0] ? lp[0] : lp[1]);
-        if (top == -INFINITY) top = 0.0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        if (j[u] < 0) lp[u] = -INFINITY;
+        s[u] = j[u] >= 0 && j[u] < a.V ? Elem<XT>::load(row + j[u]) : -INFINITY;
+        L.s[lane + 64 * u] = s[u];
+    }
+    // Which entries repeat another's index: everyone writes its number where its index' lowest bits say and reads back who
+    // stands there.  Itself: it stands for its index.  Another with this index: it repeats that one.  Else once more.
+    bool own[2] = {false, false}, open[2] = {j[0] >= 0, j[1] >= 0}, twice = false;
+    while (__ballot(open[0] || open[1])) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (open[u]) L.slot[j[u] & 2047] = (uint16_t)(lane + 64 * u);
+        lg_wave_sync();
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (open[u]) {
+                const int other = L.slot[j[u] & 2047];
+                if (other == lane + 64 * u) own[u] = true, open[u] = false;
+                else if (L.index[other] == j[u]) twice = true, open[u] = false;
+            }
+        lg_wave_sync();
+    }
+    double norm;
+    if constexpr (REST) {
+        norm = (double)a.teacher_lse[t];
+    } else {
+        const double top = (double)lg_shift(lg_wave_max(lg_max2((float)lp[0], (float)lp[1])));
         const double sum = wave_sum(exp(lp[0] - top) + exp(lp[1] - top));
         norm = sum == 0.0 ? 0.0 : top + log(sum);
     }
     double P = 0.0, H = 0.0, U = 0.0;
     const float m = lg_wave_max(lg_max2(s[0], s[1])), shift = lg_shift(m);
     float S = 0.f;
-    uint32_t distinct = 0;
     bool bad = false;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -666,43 +755,33 @@ __device__ __forceinline__ void lg_load_list(ListLds& L, const DistillArgs& a, i
         }
         L.p[lane + 64 * u] = (float)p[u];
         bad |= j[u] >= a.V;
+        if (REST && own[u]) S += lg_exp2((s[u] - shift) * c2);
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    // indices that stand more than once: every one of their entries gets the whole probability, one counts in S
-    float all[2] = {0.f, 0.f};
-    bool first[2] = {j[0] >= 0, j[1] >= 0};
-    for (int i = 0; i < a.k; ++i) {
-        const int at = L.index[i];
-        const float pi = L.p[i];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-            if (at == j[u]) {
-                all[u] += pi;
-                if (i < lane + 64 * u) first[u] = false;
-            }
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-        if (first[u]) {
-            S += lg_exp2((s[u] - shift) * c2);
-            ++distinct;
-        }
     P = wave_sum(P);
     H = wave_sum(H);
     U = wave_sum(U);
-    S = lg_wave_sum(S);
-    distinct = wave_sum(distinct);
+    if constexpr (REST) S = lg_wave_sum(S);
+    const int distinct = __popcll(__ballot(own[0])) + __popcll(__ballot(own[1]));
     const bool any_bad = __ballot(bad) != 0;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // all reads of L.p are done
-    L.p[lane] = all[0];
-    L.p[lane + 64] = all[1];
+    if (__ballot(twice)) {  // an index' entries all get its whole probability
+        lg_wave_sync();
+        float all[2] = {0.f, 0.f};
+        for (int i = 0; i < a.k; ++i)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (L.index[i] == j[u]) all[u] += L.p[i];
+        lg_wave_sync();
+        L.p[lane] = all[0];
+        L.p[lane + 64] = all[1];
+    }
     if (lane == 0) {
         L.P = P;
         L.H = H;
         L.U = U;
+        L.norm = norm;
         L.m = m;
         L.S = S;
-        L.distinct = (int)distinct;
+        L.distinct = distinct;
         L.bad = any_bad;
     }
 }
@@ -712,80 +791,85 @@ struct DistillStats {
     float m, f, m_all, l2;  // l2: log2 of the sum of all entries relative to m_all; -inf: nothing left
 };
 
-// u: the unlisted entries' sums (without a rest: all entries').  loss != nullptr: also the loss, in 64 bits
-__device__ __forceinline__ DistillStats lg_distill_stats(const ListLds& L, Part u, float c, bool rest, int V, float* loss) {
+// the probability that the teacher's list leaves, NaN for NaN
+__device__ __forceinline__ double lg_rest(const ListLds& L, bool rest, int V) {
+    const double r = rest && L.distinct < V ? 1.0 - L.P : 0.0;
+    return r < 0.0 ? 0.0 : r;
+}
+// u: the unlisted entries' sums (without a rest: all entries').  S: the sum of all relative to m_all
+__device__ __forceinline__ DistillStats lg_distill_stats(const ListLds& L, Part u, float c, bool rest, int V, float& S) {
     const float c2 = c * LG_LOG2E;
     DistillStats d;
-    const float top = rest ? lg_max2(u.m, L.m) : u.m;
     d.m = lg_shift(u.m);
-    d.m_all = lg_shift(top);
-    float S = u.S;  // of all
-    float other = 0.f;
-    if (rest) {
-        other = u.S * lg_exp2(lg_step(u.m, d.m_all, c2));
+    d.m_all = lg_shift(rest ? lg_max2(u.m, L.m) : u.m);
+    S = u.S;
+    if (!rest) {
+        d.f = (float)L.P / S;
+    } else {
+        const float other = u.S * lg_exp2(lg_step(u.m, d.m_all, c2));
         S = other + L.S * lg_exp2(lg_step(L.m, d.m_all, c2));
+        d.f = u.S == 0.f && S == S ? 0.f : (other / S - (float)lg_rest(L, rest, V)) / u.S;
     }
-    const bool none = S == 0.f, empty = L.distinct == 0;
-    double r = rest && L.distinct < V ? 1.0 - L.P : 0.0;
-    r = r < 0.0 ? 0.0 : r;  // NaN stays
-    d.l2 = log2f(S);
-    if (!rest) d.f = (float)L.P / S;
-    else d.f = u.S == 0.f && S == S ? 0.f : (other / S - (float)r) / u.S;
     d.f /= c;
-    if (none || empty) d.f = 0.f;
-    if (loss) {
-        const double lS = none ? 0.0 : log((double)S);
-        double value = L.H;
-        if (L.P != 0.0) value -= L.U + L.P * ((double)(lg_shift(L.m) - d.m_all) * c - lS);
-        if (rest && r != 0.0) value += r * (log(r) - (log((double)u.S) + (double)(d.m - d.m_all) * c - lS));
-        value /= (double)c * c;
-        if (empty) value = 0.0;
-        else if (L.bad) value = NAN;
-        *loss = (float)value;
+    d.l2 = log2f(S);
+    if (S == 0.f || L.distinct == 0 || (L.P == 0.0 && !rest)) {
+        d.f = 0.f;
+        d.l2 = -INFINITY;
+    } else if (L.bad) {
+        d.f = d.l2 = NAN;
     }
-    if (empty) d.l2 = -INFINITY;
-    else if (L.bad) d.f = d.l2 = NAN;
     return d;
 }
+// the row's loss, in 64 bits
+__device__ __forceinline__ float lg_distill_loss(const ListLds& L, Part u, const DistillStats& d, float S, float c, bool rest, int V) {
+    const double lS = S == 0.f ? 0.0 : log((double)S), r = lg_rest(L, rest, V);
+    double value = L.H;
+    if (L.P != 0.0) value -= L.U + L.P * ((double)(lg_shift(L.m) - d.m_all) * c - lS);
+    if (rest && r != 0.0) value += r * (log(r) - (log((double)u.S) + (double)(d.m - d.m_all) * c - lS));
+    if (L.distinct == 0) return 0.f;
+    return L.bad ? NAN : (float)(value / ((double)c * c));
+}
 
-__device__ __forceinline__ void lg_write_distill(const DistillArgs& a, int64_t t, const DistillStats& d) {
+__device__ __forceinline__ void lg_write_distill(const DistillArgs& a, int64_t t, const DistillStats& d, float norm) {
     if (!a.stats) return;
     float* s = a.stats + 4 * t;
-    s[0] = d.m, s[1] = d.f, s[2] = d.m_all, s[3] = d.l2;
+    s[0] = d.m, s[1] = d.f, s[2] = a.teacher_lse ? d.m_all : norm, s[3] = d.l2;  // without a rest m_all is m
 }
 
-// gradient of listed entry i (its weight w, the factor 1 / c inside)
-__device__ __forceinline__ float lg_listed_gradient(const ListLds& L, const DistillStats& d, int i, float c, bool rest, float w) {
-    const float q = lg_exp2((L.s[i] - d.m_all) * (c * LG_LOG2E) - d.l2);
-    return d.l2 == -INFINITY ? 0.f : ((rest ? q : (float)L.P * q) - L.p[i]) * (w / c);
+// gradient of a listed entry: the student's logit s, the teacher's probability p, the row's weight w
+__device__ __forceinline__ float lg_listed_gradient(const DistillStats& d, float s, float p, float c, float w) {
+    const float q = lg_exp2((s - d.m_all) * (c * LG_LOG2E) - d.l2);
+    return d.l2 == -INFINITY ? 0.f : (q - p) * (w / c);
 }
 
-// One bit per entry of the chunk's vectors: listed or not
+// One bit per entry of the chunk, in the order of LgChunk::spot: listed or not
 template <typename XT, int NV>
 struct LgBits {
+    static constexpr int N = LgVec<XT>::N;
     uint32_t* words;
-    __device__ __forceinline__ void zero(int per) {
-        for (int i = threadIdx.x; i < (per * LgVec<XT>::N + 31) / 32; i += blockDim.x) words[i] = 0;
+    int V;
+    __device__ static constexpr int size() { return (NV * LG_MAX_THREADS + 2) * N / 32 + 1; }
+    __device__ __forceinline__ void zero(int per) {  // by one wave
+        for (int i = threadIdx.x & 63; i < (per + 2) * N / 32 + 1; i += 64) words[i] = 0;
     }
-    __device__ __forceinline__ void set(const LgChunk<XT, NV>& chunk, const ListLds& L, int k) {
-        for (int i = threadIdx.x; i < k; i += blockDim.x) {
-            const int at = L.index[i] - chunk.head - chunk.first * LgVec<XT>::N;
-            if (L.index[i] >= chunk.head && at >= 0 && at < chunk.n * LgVec<XT>::N) atomicOr(words + at / 32, 1u << (at % 32));
-        }
+    __device__ __forceinline__ void set(const LgChunk<XT, NV>& chunk, int column) {
+        const int at = chunk.spot(column, V);
+        if (at >= 0) atomicOr(words + at / 32, 1u << (at % 32));
     }
     // takes the listed entries out of the chunk
-    __device__ __forceinline__ void clear(LgChunk<XT, NV>& chunk, const ListLds& L, int k) const {
+    __device__ __forceinline__ void clear(LgChunk<XT, NV>& chunk) const {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int j = i * (int)blockDim.x + (int)threadIdx.x;
-            if (j < chunk.n) {
-                const uint32_t bits = (words[j * LgVec<XT>::N / 32] >> (j * LgVec<XT>::N % 32)) & ((1u << LgVec<XT>::N) - 1u);
+            const int at = (chunk.place_of(i) + 1) * N;
+            if (chunk.has(i)) {
+                const uint32_t bits = (words[at / 32] >> (at % 32)) & ((1u << N) - 1u);
                 if (bits) LgVec<XT>::clear(chunk.w[i], bits);
             }
         }
-        if (chunk.edge_index >= 0)
-            for (int i = 0; i < k; ++i)
-                if (L.index[i] == chunk.edge_index) chunk.edge = -INFINITY;
+        if (chunk.edge_index >= 0) {
+            const int at = chunk.spot(chunk.edge_index, V);
+            if ((words[at / 32] >> (at % 32)) & 1u) chunk.edge = -INFINITY;
+        }
     }
 };
 
@@ -795,7 +879,7 @@ template <typename XT, int NV, bool REST, DistillMode MODE>
 __global__ __launch_bounds__(LG_MAX_THREADS) void distill_kernel(DistillArgs a) {
     __shared__ Part parts[16];
     __shared__ ListLds L;
-    __shared__ uint32_t words[REST ? NV * LG_MAX_THREADS * LgVec<XT>::N / 32 : 1];
+    __shared__ uint32_t words[REST ? LgBits<XT, NV>::size() : 1];
     const int64_t t = a.row0 + blockIdx.x / (uint32_t)a.splits;
     const int chunk_number = (int)(blockIdx.x % (uint32_t)a.splits);
     const int tid = threadIdx.x, wave = tid >> 6, waves = blockDim.x >> 6;
@@ -807,36 +891,57 @@ __global__ __launch_bounds__(LG_MAX_THREADS) void distill_kernel(DistillArgs a) 
         if (MODE != LG_SUMS && tid == 0) a.loss[t] = 0.f;
         return;
     }
+    const XT* row = static_cast<const XT*>(a.x) + t * a.stride;
     LgChunk<XT, NV> chunk;
-    chunk.load(static_cast<const XT*>(a.x) + t * a.stride, a.V, chunk_number, a.per);
-    LgBits<XT, NV> bits{words};
-    if constexpr (REST) bits.zero(a.per);
-    if constexpr (REST || MODE != LG_SUMS) {
-        if (wave == 0) lg_load_list<XT>(L, a, t);
-        __syncthreads();
-    }
+    chunk.place(row, a.V, chunk_number, a.per);
+    LgBits<XT, NV> bits{words, a.V};
+    // Where a list is to be read, the last wave does that while the others' loads are under way.  It has no entries, so
+    // that the registers of its arithmetic in 64 bits are not needed beside theirs.
+    constexpr bool LIST = MODE != LG_SUMS;
+    const int threads = (int)blockDim.x - (LIST ? 64 : 0);
+    if (!LIST || tid < threads) chunk.load(row, threads);
     if constexpr (REST) {
-        bits.set(chunk, L, a.k);
+        if (tid >= (int)blockDim.x - 64) {
+            bits.zero(a.per);
+            lg_wave_sync();
+            for (int i = tid & 63; i < a.k; i += 64) bits.set(chunk, a.top_index[t * a.k + i]);
+        }
         __syncthreads();
-        bits.clear(chunk, L, a.k);
     }
-    const float tm = chunk.max();
-    Part p = lg_wave_join<false>(chunk.template sums<false>(tm, c2), c2);
+    Part p{-INFINITY, 0.f, 0.f};
+    if (LIST && tid >= threads) {
+        lg_load_list<XT, REST>(L, a, t);
+        chunk.forget();
+    } else {
+        if constexpr (REST) bits.clear(chunk);
+        const float tm = chunk.max();
+        chunk.reread();
+        p = lg_wave_join<false>(chunk.template sums<false>(tm, c2), c2);
+        chunk.reread();
+    }
     if ((tid & 63) == 0) parts[wave] = p;
     __syncthreads();
     p = lg_parts_join<false>(parts, waves, c2);
     if constexpr (MODE == LG_SUMS) {
         if (tid == 0) a.parts[t * a.splits + chunk_number] = make_float4(p.m, p.S, 0.f, 0.f);
-    } else if constexpr (MODE == LG_LOSS) {
-        if (tid == 0) lg_write_distill(a, t, lg_distill_stats(L, p, a.c, REST, a.V, a.loss + t));
     } else {
-        const DistillStats d = lg_distill_stats(L, p, a.c, REST, a.V, tid == 0 ? a.loss + t : nullptr);
-        const float f = w * d.f;
-        if (f == 0.f) chunk.store(drow, [&](float) { return 0.f; });
-        else chunk.store(drow, [&](float v) { return f * lg_exp2((v - d.m) * c2); });
-        __syncthreads();
-        if (tid < a.k && L.index[tid] >= 0 && L.index[tid] < a.V)
-            Elem<XT>::store(drow + L.index[tid], lg_listed_gradient(L, d, tid, a.c, REST, w));
+        float S;
+        const DistillStats d = lg_distill_stats(L, p, a.c, REST, a.V, S);
+        if (tid >= (int)blockDim.x - 64) {
+            if ((tid & 63) == 0) {
+                a.loss[t] = lg_distill_loss(L, p, d, S, a.c, REST, a.V);
+                if constexpr (MODE == LG_LOSS) lg_write_distill(a, t, d, (float)L.norm);
+            }
+        } else if constexpr (MODE == LG_GRADIENT) {
+            const float f = w * d.f;
+            if (f == 0.f) chunk.store(drow, [&](float) { return 0.f; });
+            else chunk.store(drow, [&](float v) { return f * lg_exp2((v - d.m) * c2); });
+        }
+        if constexpr (MODE == LG_GRADIENT) {
+            __syncthreads();
+            if (tid < a.k && L.index[tid] >= 0 && L.index[tid] < a.V)
+                Elem<XT>::store(drow + L.index[tid], lg_listed_gradient(d, L.s[tid], L.p[tid], a.c, w));
+        }
     }
 }
 
@@ -850,16 +955,22 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a) {
         if (lane == 0) a.loss[t] = 0.f;
         return;
     }
-    lg_load_list<XT>(L, a, t);
+    lg_load_list<XT, REST>(L, a, t);
     __syncthreads();
     const float4 f = lane < a.splits ? a.parts[t * a.splits + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
     const Part p = lg_wave_join<false>(Part{f.x, f.y, 0.f}, a.c * LG_LOG2E);
-    if (lane == 0) lg_write_distill(a, t, lg_distill_stats(L, p, a.c, REST, a.V, a.loss + t));
+    if (lane == 0) {
+        float S;
+        const DistillStats d = lg_distill_stats(L, p, a.c, REST, a.V, S);
+        a.loss[t] = lg_distill_loss(L, p, d, S, a.c, REST, a.V);
+        lg_write_distill(a, t, d, (float)L.norm);
+    }
 }
 
 template <typename XT, int NV, bool REST>
 __global__ __launch_bounds__(256) void distill_bwd_kernel(DistillArgs a) {
-    __shared__ ListLds L;
+    __shared__ int index[BCQ_LOGITS_MAX_K];
+    __shared__ float prob[BCQ_LOGITS_MAX_K];
     const int64_t t = a.row0 + blockIdx.x / (uint32_t)a.splits;
     const int chunk_number = (int)(blockIdx.x % (uint32_t)a.splits);
     const int tid = threadIdx.x;
@@ -871,24 +982,33 @@ __global__ __launch_bounds__(256) void distill_bwd_kernel(DistillArgs a) {
         lg_zero_row(drow, a.V, chunk_number, a.splits);
         return;
     }
+    const int listed = tid < a.k ? a.top_index[t * a.k + tid] : -1;
     LgChunk<XT, NV> chunk;
-    chunk.load(row, a.V, chunk_number, a.per);
-    const float* s = a.stats + 4 * t;
-    const DistillStats d{s[0], s[1], s[2], s[3]};
-    if (tid < 64) lg_load_list<XT>(L, a, t);
+    chunk.place(row, a.V, chunk_number, a.per);
+    chunk.load(row, blockDim.x);
+    const float* stats = a.stats + 4 * t;
+    const DistillStats d{stats[0], stats[1], REST ? stats[2] : stats[0], stats[3]};
+    // the listed entries of this chunk are written once more: what they need is read before anything is overwritten
+    const bool mine = chunk.spot(listed, a.V) >= 0;
+    float s = 0.f, p = 0.f;
+    if (mine) {
+        s = Elem<XT>::load(row + listed);
+        const double norm = REST ? a.teacher_lse[t] : stats[2];
+        p = lg_exp2((float)(((double)a.top_logit[t * a.k + tid] * a.c - norm) * M_LOG2E));
+    }
+    if (tid < a.k) {
+        index[tid] = listed;
+        prob[tid] = p;
+    }
     __syncthreads();
     const float f = w * d.f;
     if (f == 0.f) chunk.store(drow, [&](float) { return 0.f; });
     else chunk.store(drow, [&](float v) { return f * lg_exp2((v - d.m) * c2); });
+    if (mine)  // an index that stands more than once has all its entries' probability
+        for (int i = 0; i < a.k; ++i)
+            if (index[i] == listed && i != tid) p += prob[i];
     __syncthreads();
-    // the listed entries of this chunk are written once more
-    if (tid < a.k && L.index[tid] >= 0 && L.index[tid] < a.V) {
-        const int vectors = (a.V - chunk.head) / LgVec<XT>::N;
-        const int v = L.index[tid] < chunk.head ? -1 : (L.index[tid] - chunk.head) / LgVec<XT>::N;
-        const bool edge = v < 0 || v >= vectors;
-        if (edge ? chunk_number == 0 : (v >= chunk.first && v < chunk.first + chunk.n))
-            Elem<XT>::store(drow + L.index[tid], lg_listed_gradient(L, d, tid, a.c, REST, w));
-    }
+    if (mine) Elem<XT>::store(drow + listed, lg_listed_gradient(d, s, p, a.c, w));
 }
 
 }  // namespace bcq
@@ -903,10 +1023,10 @@ struct Plan {
 
 int vector_entries(int dtype) { return dtype == BCQ_BF16 ? 8 : 4; }
 
-// For the forward passes.  Rows are cut where they do not fit a workgroup's registers, and where there are too few.
-Plan forward_plan(int64_t T, int64_t V, int dtype, int k) {
+// For the forward passes, with `most` threads of a workgroup for the entries.  Rows are cut where they do not fit a workgroup's registers, and where there are too few.
+Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most) {
     const int64_t vectors = (V + vector_entries(dtype) - 1) / vector_entries(dtype);
-    const int64_t least = (vectors + bcq::LG_MAX_NV * bcq::LG_MAX_THREADS - 1) / (bcq::LG_MAX_NV * bcq::LG_MAX_THREADS);
+    const int64_t least = (vectors + bcq::LG_MAX_NV * most - 1) / (bcq::LG_MAX_NV * most);
     int64_t splits = (512 + T - 1) / (T > 0 ? T : 1);
     const int64_t useful = (vectors + 511) / 512;
     if (splits > useful) splits = useful;
@@ -916,11 +1036,13 @@ Plan forward_plan(int64_t T, int64_t V, int dtype, int k) {
     Plan p;
     p.per = (int)((vectors + splits - 1) / splits);
     p.splits = (int)((vectors + p.per - 1) / p.per);
-    p.nv = p.per <= 2 * bcq::LG_MAX_THREADS ? 2 : p.per <= 8 * bcq::LG_MAX_THREADS ? 8 : 16;
+    p.nv = p.per <= 2 * most ? 2 : p.per <= 8 * most ? 8 : 16;
     p.threads = ((p.per + p.nv - 1) / p.nv + 63) / 64 * 64;
     if (p.threads < 256) p.threads = 256;
     return p;
 }
+Plan logprobs_plan(int64_t T, int64_t V, int dtype, int k) { return forward_plan(T, V, dtype, k, bcq::LG_MAX_THREADS); }
+Plan distill_plan(int64_t T, int64_t V, int dtype) { return forward_plan(T, V, dtype, 0, bcq::LG_MAX_THREADS - 64); }
 // For the gradients from saved statistics: nothing is joined, so chunks are small.
 constexpr int kBwdNv = 4;
 Plan backward_plan(int64_t V, int dtype) {
@@ -975,6 +1097,7 @@ hipError_t launch_logprobs_bwd(bcq::LogprobsBwdArgs a, int64_t T, const Plan& p,
 
 template <typename XT, int NV, bool REST, bcq::DistillMode MODE>
 void launch_distill_as(bcq::DistillArgs a, int64_t T, int threads, hipStream_t st) {
+    if (MODE != bcq::LG_SUMS) threads += 64;  // the list's wave
     slices(T, (int64_t)a.splits * threads, [&](int64_t row0, unsigned rows) {
         a.row0 = row0;
         BCQ_LAUNCH((bcq::distill_kernel<XT, NV, REST, MODE>), dim3(rows * a.splits), dim3(threads), 0, st, a);
@@ -1022,7 +1145,7 @@ bcq_status done(hipError_t e) { return e == hipSuccess ? BCQ_OK : BCQ_ERR_DEVICE
 // The partial sums of split rows (16 bytes a chunk), then their lists of alternatives, or the statistics between a loss
 // and its gradient (16 bytes a row).
 size_t workspace_need(int op, int64_t T, int64_t V, int k, int dtype) {
-    const Plan p = forward_plan(T, V, dtype, op == BCQ_OP_LOGPROBS_FWD ? k : 0);
+    const Plan p = op == BCQ_OP_LOGPROBS_FWD ? logprobs_plan(T, V, dtype, k) : distill_plan(T, V, dtype);
     if (p.splits == 1) return 0;
     const size_t parts = (size_t)T * p.splits * 16;
     if (op == BCQ_OP_LOGPROBS_FWD) return parts + (size_t)T * p.splits * k * 8;
@@ -1067,7 +1190,7 @@ bcq_status bcq_logprobs_fwd(const void* logits, int dtype, int64_t T, int64_t V,
     if (s != BCQ_OK) return s;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    const Plan p = forward_plan(T, V, dtype, k);
+    const Plan p = logprobs_plan(T, V, dtype, k);
     float4* parts = static_cast<float4*>(workspace);
     const bcq::LogprobsArgs a{logits, row_stride, tokens, 1.0f / temperature, (int)V, k, p.splits, p.per, 0, logp, entropy, lse, stats,
                               top_logit, top_logp, top_index, parts, reinterpret_cast<uint64_t*>(parts + T * p.splits)};
@@ -1163,7 +1286,7 @@ bcq_status bcq_distill_fwd(const void* logits, int dtype, int64_t T, int64_t V, 
     if (w != BCQ_OK) return w;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    const Plan p = forward_plan(T, V, dtype, 0);
+    const Plan p = distill_plan(T, V, dtype);
     bcq::DistillArgs d = distill_args(a);
     d.loss = loss;
     d.stats = stats;
@@ -1209,7 +1332,7 @@ bcq_status bcq_distill_fwd_bwd(const void* logits, int dtype, int64_t T, int64_t
     if (s != BCQ_OK) return s;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    const Plan p = forward_plan(T, V, dtype, 0);
+    const Plan p = distill_plan(T, V, dtype);
     bcq::DistillArgs d = distill_args(a);
     d.weight = weight;
     d.loss = loss;
