@@ -21,6 +21,7 @@ constexpr int LG_MAX_NV = 16;          // vectors per thread at most
 constexpr int LG_MAX_SPLITS = 64;      // chunks per row at most: a wave joins them, one per lane
 constexpr int LG_CANDIDATES = 1024;    // entries that are ranked against each other
 constexpr int LG_JOIN_CANDIDATES = 2048;
+constexpr int LG_SLOTS = 4;            // threads of a wave whose entries are searched for candidates at once
 
 __device__ __forceinline__ float lg_exp2(float v) { return __builtin_amdgcn_exp2f(v); }
 // The larger of numbers, NaN left out (fmaxf would first quieten its operands, an instruction each)
@@ -41,6 +42,9 @@ __device__ __forceinline__ float lg_unkey(uint32_t key) {
 }
 // value and index as one number: the larger value first, then the lower index
 __device__ __forceinline__ uint64_t lg_entry(float v, int index) { return ((uint64_t)lg_key(v) << 32) | (uint32_t)~index; }
+
+// what the lanes of a wave wrote to LDS is there for its other lanes
+__device__ __forceinline__ void lg_wave_sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
 // ---- reductions: over the 16 lanes of a row, and over a wave; every lane gets the result
 template <int CTRL>
@@ -67,11 +71,12 @@ __device__ __forceinline__ float lg_wave_sum(float v) {
     return (lg_lane(v, 0) + lg_lane(v, 16)) + (lg_lane(v, 32) + lg_lane(v, 48));
 }
 
-// Sums of a part of a row: S = sum 2^d, E = sum 2^d d, d = (x - m) c2, m the part's maximum (0 where it holds nothing).
+// Sums of a part of a row: S = sum 2^d, E = sum 2^d d, d = (x - m) c2.  m is the part's maximum or a value near it: S lies
+// between 2^-32 and 2^32 or so; -inf where the part holds nothing.
 struct Part {
     float m, S, E;
 };
-// the maximum as a shift
+// as a shift
 __device__ __forceinline__ float lg_shift(float m) { return m == -INFINITY ? 0.f : m; }
 // log2 of the factor from shift m to shift M >= m; far below what a sum can feel it stays finite (products with E)
 __device__ __forceinline__ float lg_step(float m, float M, float c2) { return fmaxf((m - M) * c2, -16384.f); }
@@ -213,6 +218,7 @@ struct LgChunk {
     __device__ __forceinline__ int column(int i, int e) const { return head + (first + place_of(i)) * Vec::N + e; }
     __device__ __forceinline__ bool any(int i) const { return i * threads < n; }  // the same in all lanes
 
+    // the thread's maximum (-inf for none)
     __device__ __forceinline__ float max() const {
         float m = edge;
 #pragma unroll
@@ -239,46 +245,57 @@ struct LgChunk {
 #pragma unroll
             for (int u = 0; u < 4; ++u) asm volatile("" : "+v"(w[i][u]));
     }
-    // sums relative to the thread's own maximum
-    template <bool ENT>
-    __device__ __forceinline__ Part sums(float m, float c2) const {
-        const float shift = lg_shift(m);
+    // The thread's sums, and its maximum (MAX), in one pass: the shift is the maximum of the first vector alone, which is an
+    // entry of the row and mostly near enough to the others.  Where it is not (nothing but masks in the first vector, entries
+    // far above it, NaN) a second pass takes the true maximum.  (d as one multiply-add, x c2 - fl(m c2), would save an
+    // instruction, but the row's maximum itself would then not have d = 0.)
+    template <bool ENT, bool MAX>
+    __device__ __forceinline__ Part sums(float c2, float& top) {
+        float m = edge;
+        if (any(0))
+#pragma unroll
+            for (int e = 0; e < Vec::N; e += 2) m = lg_max3(m, Vec::get(w[0], e), Vec::get(w[0], e + 1));
+        top = lg_max2(m, -INFINITY);
+        m = lg_shift(top);
         Part p{m, 0.f, 0.f};
         float S2 = 0.f;
-        auto one = [&](float x, float& S) {
-            const float d = (x - shift) * c2, e = lg_exp2(d);
+        auto add = [&](float d, float& S) {
+            const float e = lg_exp2(d);
             S += e;
             if constexpr (ENT) p.E = fmaf(e, lg_max2(d, -16384.f), p.E);
         };
-        one(edge, p.S);
+        add((edge - m) * c2, p.S);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (any(i))
 #pragma unroll
                 for (int e = 0; e < Vec::N; e += 2) {
-                    one(Vec::get(w[i], e), p.S);
-                    one(Vec::get(w[i], e + 1), S2);
+                    const float x = Vec::get(w[i], e), y = Vec::get(w[i], e + 1);
+                    add((x - m) * c2, p.S);
+                    add((y - m) * c2, S2);
+                    if (MAX && i > 0) top = lg_max3(top, x, y);
                 }
         p.S += S2;
-        return p;
-    }
-    // f(value, column) of every entry of this thread for which keep(value)
-    template <typename K, typename F>
-    __device__ __forceinline__ void each(K keep, F f) const {
-        if (edge_index >= 0 && keep(edge)) f(edge, edge_index);
+        reread();
+        if (!(p.S < 0x1p32f && p.S > 0x1p-32f)) {
+            top = max();
+            p = Part{top, 0.f, 0.f};
+            m = lg_shift(top);
+            add((edge - m) * c2, p.S);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (any(i) && has(i)) {
-                float m = -INFINITY;
+            for (int i = 0; i < NV; ++i)
+                if (any(i)) {
+                    uint32_t v[4];
 #pragma unroll
-                for (int e = 0; e < Vec::N; e += 2) m = lg_max3(m, Vec::get(w[i], e), Vec::get(w[i], e + 1));
-                if (keep(m))
-#pragma unroll
-                    for (int e = 0; e < Vec::N; ++e) {
-                        const float x = Vec::get(w[i], e);
-                        if (keep(x)) f(x, column(i, e));
+                    for (int u = 0; u < 4; ++u) {
+                        v[u] = w[i][u];
+                        asm volatile("" : "+v"(v[u]));
                     }
-            }
+#pragma unroll
+                    for (int e = 0; e < Vec::N; ++e) add((Vec::get(v, e) - m) * c2, p.S);
+                }
+        }
+        return p;
     }
     // f(value, column) of the thread's entries, read from memory once more
     template <typename F>
@@ -367,40 +384,40 @@ __device__ __forceinline__ void lg_write_top(const LogprobsArgs& a, int64_t t, i
     if (a.top_logp) a.top_logp[at] = p.S == 0.f ? -INFINITY : (v - lg_shift(p.m)) * a.c - l2 * LG_LN2;
 }
 
-// put(rank, entry) for the k first of the n entries in `list` by rank, and entry 0 for ranks beyond n.  Eight lanes share a
-// candidate, each comparing it with an eighth of the others.
+// put(rank, entry) for the k first of the n entries in `list` by rank, and entry 0 for ranks beyond n.  list[n] is written.
 template <typename F>
-__device__ __forceinline__ void lg_rank(const uint64_t* list, int n, int k, F put) {
-    const int part = threadIdx.x & 7, groups = blockDim.x >> 3;
-    for (int first = 0; first < n; first += groups) {
-        const int i = first + (int)(threadIdx.x >> 3);
-        const uint64_t mine = list[i < n ? i : 0];
+__device__ __forceinline__ void lg_rank(uint64_t* list, int n, int k, F put) {
+    if (threadIdx.x == 0) list[n] = 0;  // the entries are read in pairs
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const uint64_t mine = list[i];
         uint32_t rank = 0;
 #pragma unroll 4
-        for (int j = part; j < n; j += 8) rank += list[j] > mine ? 1u : 0u;
-        rank += dpp_move<DPP_XOR1>(rank);
-        rank += dpp_move<DPP_XOR2>(rank);
-        rank += dpp_move<DPP_HALF_MIRROR>(rank);
-        if (part == 0 && i < n && (int)rank < k) put((int)rank, mine);
+        for (int j = 0; j < n; j += 2) {
+            const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(list + j);
+            rank += (two.x > mine ? 1u : 0u) + (two.y > mine ? 1u : 0u);
+        }
+        if ((int)rank < k) put((int)rank, mine);
     }
     for (int r = n + (int)threadIdx.x; r < k; r += blockDim.x) put(r, (uint64_t)0);
 }
 
 struct TopLds {
     alignas(16) float max[LG_MAX_THREADS];  // of every thread
-    uint64_t list[LG_CANDIDATES];
+    alignas(16) uint64_t list[LG_CANDIDATES + 2];
+    uint4 words[16 * LG_SLOTS * LG_MAX_NV];  // some threads' entries, for every wave
+    int from[16][LG_SLOTS];                  // which threads
     uint32_t counts[2][16];
+    uint32_t low, high;          // keys: k entries reach `low`, none reaches `high`
     int n;
 };
 
-// The candidates for a chunk's k best in lds.list, and their number.  The threads are cut into 64 R groups, R the least power
-// of two with 32 R >= k.  At least k groups have a maximum that reaches the k-th largest of the groups' maxima, so that value
-// is a lower bound of the k-th entry, and few entries exceed it: with entries in random order -64 R ln(1 - k / (64 R)), 24 for
-// the 20 best, 74 for 64.  The bound only has to be low enough, so its search by halving stops early.
-// Called by all threads after lds.max is written and a barrier; lds.n is 0.
-template <typename XT, int NV>
-__device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>& chunk, const XT* row, int V, float tm, int k) {
-    const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+// The search for the candidates' bound, by one wave.  The threads are cut into 64 R groups, R the least power of two with
+// 32 R >= k.  At least k groups have a maximum that reaches the k-th largest of the groups' maxima, so that value is a lower
+// bound of the k-th entry, and few entries exceed it: with entries in random order -64 R ln(1 - k / (64 R)), 24 for the 20
+// best, 74 for 64.  The bound only has to be low enough, so its search by halving stops early.
+__device__ __forceinline__ void lg_bound(TopLds& lds, int k) {
+    const int lane = threadIdx.x & 63;
     float group[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     for (int i = lane; i < (int)blockDim.x / 4; i += 64) {
         const float4 q = reinterpret_cast<const float4*>(lds.max)[i];
@@ -412,45 +429,100 @@ __device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>&
     if (k <= 64) {
         group[0] = lg_max2(group[0], group[2]);
         group[1] = lg_max2(group[1], group[3]);
-        group[2] = group[3] = -INFINITY;
-        if (k <= 32) {
-            group[0] = lg_max2(group[0], group[1]);
-            group[1] = -INFINITY;
-        }
+        if (k <= 32) group[0] = lg_max2(group[0], group[1]);
     }
     uint32_t key[4], low = lg_key(-INFINITY);
-    float most = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        most = lg_max2(most, group[u]);
-        key[u] = lg_key(group[u]);
-    }
-    uint32_t high = lg_key(lg_wave_max(most)) + 1;  // no entry reaches it
+    for (int u = 0; u < 4; ++u) key[u] = lg_key(group[u]);
+    const float most = lg_max2(lg_max2(group[0], group[1]), lg_max2(group[2], group[3]));
+    const uint32_t high = lg_key(lg_wave_max(most)) + 1;
     auto reached = [&](uint32_t at) {
         uint32_t c = (uint32_t)__popcll(__ballot(key[0] >= at));
         if (k > 32) c += (uint32_t)__popcll(__ballot(key[1] >= at));
         if (k > 64) c += (uint32_t)(__popcll(__ballot(key[2] >= at)) + __popcll(__ballot(key[3] >= at)));
         return (int)c;
     };
-    {
-        int reach = 256;
-        uint32_t over = high, step = 1u << 21;  // the first steps down from the maximum: a quarter of it each, doubled
-        while (over - low > 1 && reach > k + 8 + k / 4) {
-            const uint32_t half = low + (over - low) / 2, down = over - low > step ? over - step : half;
-            const uint32_t mid = reach == 256 && down > half ? down : half;
-            const int c = reached(mid);
-            if (step < 1u << 30) step *= 2;
-            if (c >= k) low = mid, reach = c;
-            else over = mid;
+    bool found = false;
+    uint32_t over = high, step = 1u << 21;  // down from the maximum, by a quarter of its power of two first, then by twice as much
+    while (over - low > 1) {
+        const uint32_t half = low + (over - low) / 2, down = over - low > step ? over - step : half;
+        const uint32_t mid = !found && down > half ? down : half;
+        const int c = reached(mid);
+        if (step < 1u << 30) step *= 2;
+        if (c >= k) {
+            low = mid;
+            found = true;
+            if (c <= k + 8 + k / 4) break;
+        } else {
+            over = mid;
         }
     }
+    if (lane == 0) {
+        lds.low = low;
+        lds.high = high;
+        lds.n = 0;
+    }
+}
+
+// The candidates for a chunk's k best in lds.list, and their number.  Called by all threads after lds.max is written and a
+// barrier.
+template <typename XT, int NV>
+__device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>& chunk, const XT* row, int V, float tm, int k) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    if (wave == 0) lg_bound(lds, k);
+    __syncthreads();
+    uint32_t low = lds.low, high = lds.high;
     const float bound = lg_unkey(low);
-    if (tm >= bound)
-        chunk.each([&](float x) { return x >= bound; },
-                   [&](float x, int index) {
-                       const int at = atomicAdd(&lds.n, 1);
-                       if (at < LG_CANDIDATES) lds.list[at] = lg_entry(x, index);
-                   });
+    if (chunk.edge_index >= 0 && chunk.edge >= bound) {
+        const int at = atomicAdd(&lds.n, 1);
+        if (at < LG_CANDIDATES) lds.list[at] = lg_entry(chunk.edge, chunk.edge_index);
+    }
+    // A wave takes its few threads that hold candidates some at a time: these lay their entries out, and all lanes look at one
+    // entry after another.
+    constexpr int N = LgVec<XT>::N, EACH = NV * N, TURNS = (LG_SLOTS * EACH + 63) / 64;
+    uint4* words = lds.words + wave * LG_SLOTS * NV;
+    for (uint64_t left = __ballot(tm >= bound); left;) {
+        const uint64_t below = ((uint64_t)1 << lane) - 1;
+        const int slot = __popcll(left & below);
+        const bool mine = ((left >> lane) & 1) && slot < LG_SLOTS;
+        if (mine) {
+            lds.from[wave][slot] = lane;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) words[slot * NV + i] = make_uint4(chunk.w[i][0], chunk.w[i][1], chunk.w[i][2], chunk.w[i][3]);
+        }
+        const uint64_t taken = __ballot(mine);
+        const int slots = __popcll(taken);
+        left &= ~taken;
+        lg_wave_sync();
+        float x[TURNS];
+        int place[TURNS];
+        uint64_t found[TURNS];
+        int total = 0;
+#pragma unroll
+        for (int u = 0; u < TURNS; ++u) {
+            const int e = u * 64 + lane, from = e / EACH;
+            const bool there = from < slots;
+            x[u] = there ? Elem<XT>::load(reinterpret_cast<const XT*>(words) + e) : -INFINITY;
+            place[u] = there ? e % EACH / N * chunk.threads + wave * 64 + lds.from[wave][from] : INT_MAX;
+        }
+#pragma unroll
+        for (int u = 0; u < TURNS; ++u) {
+            found[u] = __ballot(x[u] >= bound && place[u] < chunk.n);
+            total += __popcll(found[u]);
+        }
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&lds.n, total);
+        at = __builtin_amdgcn_readfirstlane(at);
+        if (at > LG_CANDIDATES) break;
+#pragma unroll
+        for (int u = 0; u < TURNS; ++u) {
+            const int here = at + __popcll(found[u] & below);
+            if (((found[u] >> lane) & 1) && here < LG_CANDIDATES)
+                lds.list[here] = lg_entry(x[u], chunk.head + (chunk.first + place[u]) * N + (u * 64 + lane) % N);
+            at += __popcll(found[u]);
+        }
+        lg_wave_sync();
+    }
     __syncthreads();
     int n = lds.n;
     if (n <= LG_CANDIDATES) return n;
@@ -520,7 +592,7 @@ __device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>&
 }
 
 template <typename XT, int NV, bool ENT, bool TOP>
-__global__ __launch_bounds__(LG_MAX_THREADS) void logprobs_kernel(LogprobsArgs a) {
+__global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80))) void logprobs_kernel(LogprobsArgs a) {
     __shared__ Part parts[16];
     __shared__ TopLds top;
     const int64_t t = a.row0 + blockIdx.x / (uint32_t)a.splits;
@@ -539,14 +611,12 @@ __global__ __launch_bounds__(LG_MAX_THREADS) void logprobs_kernel(LogprobsArgs a
     LgChunk<XT, NV> chunk;
     chunk.place(row, a.V, chunk_number, a.per);
     chunk.load(row, blockDim.x);
-    float tm = chunk.max();
-    chunk.reread();
-    Part p = lg_wave_join<ENT>(chunk.template sums<ENT>(tm, c2), c2);
+    float tm;
+    Part p = lg_wave_join<ENT>(chunk.template sums<ENT, TOP>(c2, tm), c2);
     chunk.reread();
     if ((tid & 63) == 0) parts[wave] = p;
     if constexpr (TOP) {
         top.max[tid] = tm;
-        if (tid == 0) top.n = 0;
     }
     __syncthreads();
     p = lg_parts_join<ENT>(parts, waves, c2);
@@ -557,7 +627,7 @@ __global__ __launch_bounds__(LG_MAX_THREADS) void logprobs_kernel(LogprobsArgs a
         else a.parts[t * a.splits + chunk_number] = make_float4(p.m, p.S, p.E, 0.f);
     }
     if constexpr (TOP) {
-        if (p.S != p.S) {
+        if (p.S != p.S) {  // the maxima may not be what they should
             chunk.quiet();
             tm = chunk.max();
             top.max[tid] = tm;
@@ -575,7 +645,7 @@ __global__ __launch_bounds__(LG_MAX_THREADS) void logprobs_kernel(LogprobsArgs a
 // Joins the chunks of a row: one workgroup per row
 template <typename XT, bool ENT, bool TOP>
 __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobsArgs a) {
-    __shared__ uint64_t list[TOP ? LG_JOIN_CANDIDATES : 1];
+    __shared__ alignas(16) uint64_t list[TOP ? LG_JOIN_CANDIDATES + 2 : 1];
     __shared__ int count;
     const int64_t t = a.row0 + blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -689,8 +759,6 @@ struct ListLds {
     float m, S;                 // the listed entries' maximum and sum, every index once
     int distinct, bad;          // listed indices; whether one is out of range
 };
-
-__device__ __forceinline__ void lg_wave_sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
 // By one wave alone, two entries a lane; the caller's barrier follows.  REST: the listed entries' sum is needed.
 template <typename XT, bool REST>
@@ -876,7 +944,7 @@ struct LgBits {
 // Sums of a chunk; or, of a row that is one chunk, the loss (and statistics), or loss and gradient
 enum DistillMode { LG_SUMS, LG_LOSS, LG_GRADIENT };
 template <typename XT, int NV, bool REST, DistillMode MODE>
-__global__ __launch_bounds__(LG_MAX_THREADS) void distill_kernel(DistillArgs a) {
+__global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80))) void distill_kernel(DistillArgs a) {
     __shared__ Part parts[16];
     __shared__ ListLds L;
     __shared__ uint32_t words[REST ? LgBits<XT, NV>::size() : 1];
@@ -914,9 +982,8 @@ __global__ __launch_bounds__(LG_MAX_THREADS) void distill_kernel(DistillArgs a) 
         chunk.forget();
     } else {
         if constexpr (REST) bits.clear(chunk);
-        const float tm = chunk.max();
-        chunk.reread();
-        p = lg_wave_join<false>(chunk.template sums<false>(tm, c2), c2);
+        float top;
+        p = lg_wave_join<false>(chunk.template sums<false, false>(c2, top), c2);
         chunk.reread();
     }
     if ((tid & 63) == 0) parts[wave] = p;
