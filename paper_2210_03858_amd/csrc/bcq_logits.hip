@@ -621,8 +621,8 @@ __global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80))
     __syncthreads();
     p = lg_parts_join<ENT>(parts, waves, c2);
     const bool whole = a.splits == 1;
-    const float l2 = whole ? log2f(p.S) : 0.f;
-    if (tid == 0) {
+    const float l2 = whole ? __builtin_amdgcn_logf(p.S) : 0.f;
+    if (tid == (int)blockDim.x - 64) {  // not in the first wave, which goes on with the candidates' bound
         if (whole) lg_write_row<XT>(a, t, token, p, l2);
         else a.parts[t * a.splits + chunk_number] = make_float4(p.m, p.S, p.E, 0.f);
     }
@@ -654,7 +654,7 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobsArgs a) {
     if (!ENT && !TOP && token < 0 && !a.lse) return;
     const float4 f = lane < a.splits ? a.parts[t * a.splits + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
     const Part p = lg_wave_join<ENT>(Part{f.x, f.y, f.z}, c2);
-    const float l2 = log2f(p.S);
+    const float l2 = __builtin_amdgcn_logf(p.S);
     if (tid == 0) lg_write_row<XT>(a, t, token, p, l2);
     if constexpr (TOP) {
         // The first ceil(k / splits) entries of every list are k together: the least of their last ones is a lower bound.
@@ -879,7 +879,7 @@ __device__ __forceinline__ DistillStats lg_distill_stats(const ListLds& L, Part 
         d.f = u.S == 0.f && S == S ? 0.f : (other / S - (float)lg_rest(L, rest, V)) / u.S;
     }
     d.f /= c;
-    d.l2 = log2f(S);
+    d.l2 = __builtin_amdgcn_logf(S);
     if (S == 0.f || L.distinct == 0 || (L.P == 0.0 && !rest)) {
         d.f = 0.f;
         d.l2 = -INFINITY;
