@@ -159,15 +159,25 @@ def token_logprobs(logits, tokens, temperature=1.0, entropy=False):
     """ln softmax(logits / temperature) at tokens, and the entropy of every row (None unless asked for), differentiable
     with respect to the logits.  logits [..., V] fp32 or bf16; tokens [...] int64, negative where there is none (0, no
     gradient)."""
+    args = (logits, tokens) if logits.dim() == 2 else (_rows(logits), _flat(tokens, ()))
+    out = None if torch.compiler.is_compiling() else B._try_native("token_logprobs", *args, float(temperature), bool(entropy))
+    if out is None:
+        out = TokenLogprobsFunction.apply(_rows(logits), _flat(tokens, ()), float(temperature), bool(entropy))
+    if logits.dim() == 2:
+        return tuple(out)
     shape = logits.shape[:-1]
-    logp, H = TokenLogprobsFunction.apply(_rows(logits), _flat(tokens, ()), float(temperature), bool(entropy))
-    return logp.reshape(shape), None if H is None else H.reshape(shape)
+    return out[0].reshape(shape), None if out[1] is None else out[1].reshape(shape)
 
 
 def distill_loss(logits, top_logit, top_index, teacher_lse=None, temperature=1.0):
     """Loss [...] of logits [..., V] against a teacher's list (top_logit fp32 and top_index int32 [..., k]), with
     teacher_lse [...] also against the rest of its vocabulary; differentiable with respect to the logits."""
-    shape, k = logits.shape[:-1], top_index.shape[-1]
-    loss = DistillLossFunction.apply(_rows(logits), _flat(top_logit, (k,)), _flat(top_index, (k,)),
-                                     _flat(teacher_lse, ()), float(temperature))
-    return loss.reshape(shape)
+    def rows():
+        k = top_index.shape[-1]
+        return _rows(logits), _flat(top_logit, (k,)), _flat(top_index, (k,)), _flat(teacher_lse, ())
+
+    args = (logits, top_logit, top_index, teacher_lse) if logits.dim() == 2 else rows()
+    loss = None if torch.compiler.is_compiling() else B._try_native("distill_loss", *args, float(temperature))
+    if loss is None:
+        loss = DistillLossFunction.apply(*rows(), float(temperature))
+    return loss if logits.dim() == 2 else loss.reshape(logits.shape[:-1])

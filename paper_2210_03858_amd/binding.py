@@ -644,6 +644,10 @@ def bcq_logprobs_fwd(logits, tokens=None, k=0, temperature=1.0, entropy=False, l
     logits [T, V] fp32 or bf16 (rows may lie apart); tokens [T] int64, negative for none.  k > 0: the k best entries
     (top_index int32, top_logit, top_logp, each [T, k]).  stats: what bcq_logprobs_bwd needs.  out: a Logprobs with the
     tensors to fill instead; its fields say what is computed."""
+    if out is None and workspace is None:
+        new = _try_native("logprobs_fwd", logits, tokens, k, float(temperature), entropy, lse, stats)
+        if new is not None:
+            return Logprobs._make(new)
     T, V, stride = _table(logits, "logits")
     dt = _act_dtype(logits)
     k = int(k)
@@ -741,6 +745,10 @@ def bcq_distill_fwd_bwd(logits, top_logit, top_index, weight=None, teacher_lse=N
                         workspace=None):
     """Loss [T] and the gradient of sum(weight * loss) in one call -> (loss, dlogits); rows of weight 0 are skipped.
     dlogits may be logits itself."""
+    if loss is None and dlogits is None and workspace is None:
+        new = _try_native("distill_fwd_bwd", logits, top_logit, top_index, weight, teacher_lse, float(temperature))
+        if new is not None:
+            return new
     T, V, stride = _table(logits, "logits")
     dt = _act_dtype(logits)
     k = _list(top_logit, top_index, teacher_lse, T)

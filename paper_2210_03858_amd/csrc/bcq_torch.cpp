@@ -326,6 +326,197 @@ py::object linear(const Tensor& x, const Tensor& alpha_train, const OptTensor& a
     }
 }
 
+// ---- operators on logits ------------------------------------------------------------------------------------------
+// A table of logits [T, V] on the current device: rows of contiguous entries, any distance from row to row.
+struct Table {
+    int64_t T = 0, V = 0, stride = 0;
+    int code = -1;
+    bool ok = false;
+};
+Table table(const Tensor& t) {
+    Table a;
+    if (!t.defined() || t.dim() != 2 || !t.is_cuda() || t.layout() != at::kStrided || t.is_neg() ||
+        t.key_set().has(c10::DispatchKey::Python) || t.get_device() != c10::hip::current_device())
+        return a;
+    a.T = t.size(0);
+    a.V = t.size(1);
+    a.code = act_code(t);
+    a.stride = a.T > 1 ? t.stride(0) : a.V;
+    a.ok = a.T > 0 && a.V > 0 && a.code >= 0 && (a.V == 1 || t.stride(1) == 1) && a.stride >= a.V;
+    return a;
+}
+bool vector_of(const OptTensor& t, at::ScalarType type, at::IntArrayRef shape) { return !t || (plain(*t, type, shape) && !t->is_neg()); }
+bool list_ok(const Table& a, const Tensor& top_logit, const Tensor& top_index, const OptTensor& teacher_lse, int64_t* k) {
+    if (!top_index.defined() || top_index.dim() != 2) return false;
+    *k = top_index.size(1);
+    return vector_of(top_index, at::kInt, {a.T, *k}) && vector_of(top_logit, at::kFloat, {a.T, *k}) && vector_of(teacher_lse, at::kFloat, {a.T});
+}
+// Scratch of one call as for the layers; undefined where none is needed
+bool logits_scratch(int op, const Table& a, int64_t k, const Tensor& like, Tensor* ws) {
+    size_t need = 0;
+    if (bcq_logits_workspace_bytes(op, a.T, a.V, (int)k, a.code, &need) != BCQ_OK) return false;
+    if (need) *ws = at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+    return true;
+}
+void* raw(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+float* floats(const Tensor& t) { return static_cast<float*>(raw(t)); }
+size_t room(const Tensor& t) { return t.defined() ? (size_t)t.numel() : 0; }
+
+py::object logprobs_fwd(const Tensor& logits, const OptTensor& tokens, int64_t k, double temperature, bool entropy, bool lse, bool stats) {
+    const Table a = table(logits);
+    if (!a.ok || k < 0 || k > BCQ_LOGITS_MAX_K || (tokens && !plain(*tokens, at::kLong, {a.T}))) return py::none();
+    Tensor out[7], ws;
+    if (!logits_scratch(BCQ_OP_LOGPROBS_FWD, a, k, logits, &ws)) return py::none();
+    const auto options = logits.options().dtype(at::kFloat).requires_grad(false);
+    if (tokens) out[0] = at::empty({a.T}, options);
+    if (entropy) out[1] = at::empty({a.T}, options);
+    if (lse) out[2] = at::empty({a.T}, options);
+    if (stats) out[3] = at::empty({a.T, 2}, options);
+    if (k) {
+        out[4] = at::empty({a.T, k}, options.dtype(at::kInt));
+        out[5] = at::empty({a.T, k}, options);
+        out[6] = at::empty({a.T, k}, options);
+    }
+    const bcq_status st = unlocked([&] {
+        return bcq_logprobs_fwd(logits.data_ptr(), a.code, a.T, a.V, a.stride, static_cast<const int64_t*>(ptr(tokens)), (float)temperature,
+                                (int)k, floats(out[0]), floats(out[1]), floats(out[2]), floats(out[3]), static_cast<int32_t*>(raw(out[4])),
+                                floats(out[5]), floats(out[6]), raw(ws), room(ws), current_stream());
+    });
+    if (st != BCQ_OK) return py::none();
+    py::tuple result(7);
+    for (int i = 0; i < 7; ++i) result[i] = out[i].defined() ? py::cast(out[i]) : py::object(py::none());
+    return std::move(result);
+}
+
+py::object distill_fwd_bwd(const Tensor& logits, const Tensor& top_logit, const Tensor& top_index, const OptTensor& weight,
+                           const OptTensor& teacher_lse, double temperature) {
+    const Table a = table(logits);
+    int64_t k = 0;
+    Tensor ws;
+    if (!a.ok || !list_ok(a, top_logit, top_index, teacher_lse, &k) || !vector_of(weight, at::kFloat, {a.T}) ||
+        !logits_scratch(BCQ_OP_DISTILL_FWD_BWD, a, k, logits, &ws))
+        return py::none();
+    const auto options = logits.options().requires_grad(false);
+    const Tensor loss = at::empty({a.T}, options.dtype(at::kFloat)), dlogits = at::empty({a.T, a.V}, options);
+    const bcq_status st = unlocked([&] {
+        return bcq_distill_fwd_bwd(logits.data_ptr(), a.code, a.T, a.V, a.stride, floats(top_logit), static_cast<const int32_t*>(raw(top_index)),
+                                   (int)k, static_cast<const float*>(ptr(teacher_lse)), (float)temperature,
+                                   static_cast<const float*>(ptr(weight)), floats(loss), dlogits.data_ptr(), a.V, raw(ws), room(ws),
+                                   current_stream());
+    });
+    return st == BCQ_OK ? py::object(py::make_tuple(loss, dlogits)) : py::none();
+}
+
+// a gradient that arrives expanded or strided, as the dense tensor that the C entry points take
+Tensor dense(const Tensor& t, at::IntArrayRef shape) {
+    const Tensor d = t.contiguous();
+    TORCH_CHECK_VALUE(plain(d, at::kFloat, shape), "the gradient must be a float32 cuda tensor");
+    return d;
+}
+
+struct TokenLogprobsNode : public torch::autograd::Function<TokenLogprobsNode> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& logits, const Tensor& tokens,
+                                                  double temperature, bool entropy) {
+        const Table a = table(logits);
+        Tensor ws;
+        if (!a.ok || !plain(tokens, at::kLong, {a.T}) || !logits_scratch(BCQ_OP_LOGPROBS_FWD, a, 0, logits, &ws)) throw Refused{};
+        const auto options = logits.options().dtype(at::kFloat).requires_grad(false);
+        const Tensor logp = at::empty({a.T}, options), stats = at::empty({a.T, 2}, options);
+        const Tensor H = entropy ? at::empty({a.T}, options) : Tensor();
+        if (bcq_logprobs_fwd(logits.data_ptr(), a.code, a.T, a.V, a.stride, tokens.data_ptr<int64_t>(), (float)temperature, 0, floats(logp),
+                             floats(H), nullptr, floats(stats), nullptr, nullptr, nullptr, raw(ws), room(ws), current_stream()) != BCQ_OK)
+            throw Refused{};
+        ctx->save_for_backward({logits, tokens, stats, H});
+        ctx->saved_data["temperature"] = temperature;
+        ctx->set_materialize_grads(false);
+        if (!entropy) return {logp};
+        return {logp, H};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, const torch::autograd::variable_list& grads) {
+        const auto saved = ctx->get_saved_variables();
+        const Tensor &logits = saved[0], &tokens = saved[1], &stats = saved[2], &H = saved[3];
+        const Tensor d_logp = grads[0], d_H = grads.size() > 1 ? grads[1] : Tensor();
+        if (!d_logp.defined() && !d_H.defined()) return {Tensor(), Tensor(), Tensor(), Tensor()};
+        const Table a = table(logits);
+        TORCH_CHECK_VALUE(a.ok, "logits must be a table on the current device");
+        const Tensor dlogp = d_logp.defined() ? dense(d_logp, {a.T}) : Tensor();
+        const Tensor dH = d_H.defined() ? dense(d_H, {a.T}) : Tensor();
+        const Tensor dx = at::empty({a.T, a.V}, logits.options().requires_grad(false));
+        const bcq_status st = bcq_logprobs_bwd(logits.data_ptr(), a.code, a.T, a.V, a.stride, dlogp.defined() ? tokens.data_ptr<int64_t>() : nullptr,
+                                               (float)ctx->saved_data["temperature"].toDouble(), floats(stats), floats(dlogp),
+                                               dH.defined() ? floats(H) : nullptr, floats(dH), dx.data_ptr(), a.V, current_stream());
+        if (st != BCQ_OK) raise_bcq_error(st, "bcq_logprobs_bwd");
+        return {dx, Tensor(), Tensor(), Tensor()};
+    }
+};
+
+struct DistillLossNode : public torch::autograd::Function<DistillLossNode> {
+    static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& logits, const Tensor& top_logit, const Tensor& top_index,
+                          const Tensor& teacher_lse, double temperature) {
+        const Table a = table(logits);
+        int64_t k = 0;
+        Tensor ws;
+        if (!a.ok || !list_ok(a, top_logit, top_index, teacher_lse.defined() ? OptTensor(teacher_lse) : OptTensor(), &k) ||
+            !logits_scratch(BCQ_OP_DISTILL_FWD, a, k, logits, &ws))
+            throw Refused{};
+        const auto options = logits.options().dtype(at::kFloat).requires_grad(false);
+        const Tensor loss = at::empty({a.T}, options), stats = at::empty({a.T, 4}, options);
+        if (bcq_distill_fwd(logits.data_ptr(), a.code, a.T, a.V, a.stride, floats(top_logit), static_cast<const int32_t*>(raw(top_index)), (int)k,
+                            floats(teacher_lse), (float)temperature, floats(loss), floats(stats), raw(ws), room(ws), current_stream()) != BCQ_OK)
+            throw Refused{};
+        ctx->save_for_backward({logits, top_logit, top_index, teacher_lse, stats});
+        ctx->saved_data["temperature"] = temperature;
+        return loss;
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, const torch::autograd::variable_list& grads) {
+        const auto saved = ctx->get_saved_variables();
+        const Tensor &logits = saved[0], &top_logit = saved[1], &top_index = saved[2], &teacher_lse = saved[3], &stats = saved[4];
+        const Table a = table(logits);
+        TORCH_CHECK_VALUE(a.ok, "logits must be a table on the current device");
+        const Tensor dloss = dense(grads[0], {a.T});
+        const Tensor dx = at::empty({a.T, a.V}, logits.options().requires_grad(false));
+        const bcq_status st = bcq_distill_bwd(logits.data_ptr(), a.code, a.T, a.V, a.stride, floats(top_logit),
+                                              static_cast<const int32_t*>(raw(top_index)), (int)top_index.size(1), floats(teacher_lse),
+                                              (float)ctx->saved_data["temperature"].toDouble(), floats(stats), floats(dloss), dx.data_ptr(),
+                                              a.V, current_stream());
+        if (st != BCQ_OK) raise_bcq_error(st, "bcq_distill_bwd");
+        return {dx, Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+
+bool plain_mode(const Tensor& logits) {
+    return !c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode) && !torch::jit::tracer::isTracing() &&
+           !c10::impl::TorchDispatchModeTLS::any_modes_set() && logits.defined() && !transformed(logits);
+}
+
+// (logp, entropy or None), or None: the caller takes the Python node.  logits is a table, tokens [T].
+py::object token_logprobs(const Tensor& logits, const Tensor& tokens, double temperature, bool entropy) {
+    if (!plain_mode(logits) || !table(logits).ok) return py::none();
+    try {
+        torch::autograd::variable_list out;
+        {
+            py::gil_scoped_release release;
+            out = TokenLogprobsNode::apply(logits, tokens, temperature, entropy);
+        }
+        return py::make_tuple(out[0], out.size() > 1 ? py::cast(out[1]) : py::object(py::none()));
+    } catch (const Refused&) {
+        return py::none();
+    }
+}
+py::object distill_loss(const Tensor& logits, const Tensor& top_logit, const Tensor& top_index, const OptTensor& teacher_lse, double temperature) {
+    if (!plain_mode(logits) || !table(logits).ok || top_logit.requires_grad() || (teacher_lse && teacher_lse->requires_grad())) return py::none();
+    try {
+        Tensor loss;
+        {
+            py::gil_scoped_release release;
+            loss = DistillLossNode::apply(logits, top_logit, top_index, teacher_lse.value_or(Tensor()), temperature);
+        }
+        return py::cast(loss);
+    } catch (const Refused&) {
+        return py::none();
+    }
+}
+
 // Arguments of other types reach the second form, so that the caller need not catch the TypeError of a failed conversion
 // and take one that user code raised inside the call (a saved-tensor hook) for it.
 template <typename F>
@@ -345,4 +536,8 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
     define(m, "pack_transposed", &pack_transposed);
     define(m, "pack_decode", &pack_decode);
     define(m, "linear", &linear);
+    define(m, "logprobs_fwd", &logprobs_fwd);
+    define(m, "distill_fwd_bwd", &distill_fwd_bwd);
+    define(m, "token_logprobs", &token_logprobs);
+    define(m, "distill_loss", &distill_loss);
 }
