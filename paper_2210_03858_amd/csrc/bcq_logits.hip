@@ -384,28 +384,34 @@ __device__ __forceinline__ void lg_write_top(const LogprobsArgs& a, int64_t t, i
     if (a.top_logp) a.top_logp[at] = p.S == 0.f ? -INFINITY : (v - lg_shift(p.m)) * a.c - l2 * LG_LN2;
 }
 
-// put(rank, entry) for the k first of the n entries in `list` by rank, and entry 0 for ranks beyond n.  list[n] is written.
+// put(rank, entry) for the k first of the n entries in `list` by rank, and entry 0 for ranks beyond n.  Four lanes share an
+// entry, each comparing it with a quarter of the others, two at a time.  list[n] to list[n + 7] are written.
 template <typename F>
 __device__ __forceinline__ void lg_rank(uint64_t* list, int n, int k, F put) {
-    if (threadIdx.x == 0) list[n] = 0;  // the entries are read in pairs
+    if (threadIdx.x < 8) list[n + threadIdx.x] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const uint64_t mine = list[i];
+    const int part = threadIdx.x & 3, groups = blockDim.x >> 2;
+    for (int first = 0; first < n; first += groups) {
+        const int i = first + (int)(threadIdx.x >> 2);
+        const uint64_t mine = list[i < n ? i : n];
         uint32_t rank = 0;
 #pragma unroll 4
-        for (int j = 0; j < n; j += 2) {
+        for (int j = 2 * part; j < n; j += 8) {
             const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(list + j);
             rank += (two.x > mine ? 1u : 0u) + (two.y > mine ? 1u : 0u);
         }
-        if ((int)rank < k) put((int)rank, mine);
+        rank += dpp_move<DPP_XOR1>(rank);
+        rank += dpp_move<DPP_XOR2>(rank);
+        if (part == 0 && i < n && (int)rank < k) put((int)rank, mine);
     }
     for (int r = n + (int)threadIdx.x; r < k; r += blockDim.x) put(r, (uint64_t)0);
 }
 
+template <int NV>
 struct TopLds {
     alignas(16) float max[LG_MAX_THREADS];  // of every thread
-    alignas(16) uint64_t list[LG_CANDIDATES + 2];
-    uint4 words[16 * LG_SLOTS * LG_MAX_NV];  // some threads' entries, for every wave
+    alignas(16) uint64_t list[LG_CANDIDATES + 8];
+    uint4 words[16 * LG_SLOTS * NV];          // some threads' entries, for every wave
     int from[16][LG_SLOTS];                  // which threads
     uint32_t counts[2][16];
     uint32_t low, high;          // keys: k entries reach `low`, none reaches `high`
@@ -416,7 +422,8 @@ struct TopLds {
 // 32 R >= k.  At least k groups have a maximum that reaches the k-th largest of the groups' maxima, so that value is a lower
 // bound of the k-th entry, and few entries exceed it: with entries in random order -64 R ln(1 - k / (64 R)), 24 for the 20
 // best, 74 for 64.  The bound only has to be low enough, so its search by halving stops early.
-__device__ __forceinline__ void lg_bound(TopLds& lds, int k) {
+template <int NV>
+__device__ __forceinline__ void lg_bound(TopLds<NV>& lds, int k) {
     const int lane = threadIdx.x & 63;
     float group[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     for (int i = lane; i < (int)blockDim.x / 4; i += 64) {
@@ -452,7 +459,7 @@ __device__ __forceinline__ void lg_bound(TopLds& lds, int k) {
         if (c >= k) {
             low = mid;
             found = true;
-            if (c <= k + 8 + k / 4) break;
+            if (c <= k + 2 + k / 16) break;
         } else {
             over = mid;
         }
@@ -467,7 +474,7 @@ __device__ __forceinline__ void lg_bound(TopLds& lds, int k) {
 // The candidates for a chunk's k best in lds.list, and their number.  Called by all threads after lds.max is written and a
 // barrier.
 template <typename XT, int NV>
-__device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>& chunk, const XT* row, int V, float tm, int k) {
+__device__ __forceinline__ int lg_candidates(TopLds<NV>& lds, const LgChunk<XT, NV>& chunk, const XT* row, int V, float tm, int k) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     if (wave == 0) lg_bound(lds, k);
     __syncthreads();
@@ -479,10 +486,11 @@ __device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>&
     }
     // A wave takes its few threads that hold candidates some at a time: these lay their entries out, and all lanes look at one
     // entry after another.
-    constexpr int N = LgVec<XT>::N, EACH = NV * N, TURNS = (LG_SLOTS * EACH + 63) / 64;
+    constexpr int N = LgVec<XT>::N, EACH = NV * N, ALL = LG_SLOTS * EACH;
+    constexpr int TURNS = ALL >= 64 * 2 ? 2 : (ALL + 63) / 64;  // entries of a lane at a time
     uint4* words = lds.words + wave * LG_SLOTS * NV;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
     for (uint64_t left = __ballot(tm >= bound); left;) {
-        const uint64_t below = ((uint64_t)1 << lane) - 1;
         const int slot = __popcll(left & below);
         const bool mine = ((left >> lane) & 1) && slot < LG_SLOTS;
         if (mine) {
@@ -491,36 +499,37 @@ __device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>&
             for (int i = 0; i < NV; ++i) words[slot * NV + i] = make_uint4(chunk.w[i][0], chunk.w[i][1], chunk.w[i][2], chunk.w[i][3]);
         }
         const uint64_t taken = __ballot(mine);
-        const int slots = __popcll(taken);
+        const int entries = __popcll(taken) * EACH;
         left &= ~taken;
         lg_wave_sync();
-        float x[TURNS];
-        int place[TURNS];
-        uint64_t found[TURNS];
-        int total = 0;
-#pragma unroll
-        for (int u = 0; u < TURNS; ++u) {
-            const int e = u * 64 + lane, from = e / EACH;
-            const bool there = from < slots;
-            x[u] = there ? Elem<XT>::load(reinterpret_cast<const XT*>(words) + e) : -INFINITY;
-            place[u] = there ? e % EACH / N * chunk.threads + wave * 64 + lds.from[wave][from] : INT_MAX;
-        }
-#pragma unroll
-        for (int u = 0; u < TURNS; ++u) {
-            found[u] = __ballot(x[u] >= bound && place[u] < chunk.n);
-            total += __popcll(found[u]);
-        }
         int at = 0;
-        if (lane == 0) at = atomicAdd(&lds.n, total);
-        at = __builtin_amdgcn_readfirstlane(at);
-        if (at > LG_CANDIDATES) break;
+#pragma unroll 1
+        for (int e0 = 0; e0 < entries; e0 += 64 * TURNS) {
+            auto place = [&](int e) { return e % EACH / N * chunk.threads + wave * 64 + lds.from[wave][e / EACH]; };
+            float x[TURNS];
+            uint64_t found[TURNS];
+            int total = 0;
 #pragma unroll
-        for (int u = 0; u < TURNS; ++u) {
-            const int here = at + __popcll(found[u] & below);
-            if (((found[u] >> lane) & 1) && here < LG_CANDIDATES)
-                lds.list[here] = lg_entry(x[u], chunk.head + (chunk.first + place[u]) * N + (u * 64 + lane) % N);
-            at += __popcll(found[u]);
+            for (int u = 0; u < TURNS; ++u) {
+                const int e = e0 + u * 64 + lane;
+                x[u] = e < entries && place(e) < chunk.n ? Elem<XT>::load(reinterpret_cast<const XT*>(words) + e) : NAN;
+            }
+#pragma unroll
+            for (int u = 0; u < TURNS; ++u) {
+                found[u] = __ballot(x[u] >= bound);
+                total += __popcll(found[u]);
+            }
+            if (lane == 0) at = atomicAdd(&lds.n, total);
+            at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+            for (int u = 0; u < TURNS; ++u) {
+                const int here = at + __popcll(found[u] & below);
+                if (((found[u] >> lane) & 1) && here < LG_CANDIDATES)
+                    lds.list[here] = lg_entry(x[u], chunk.head + (chunk.first + place(e0 + u * 64 + lane)) * N + lane % N);
+                at += __popcll(found[u]);
+            }
         }
+        if (at > LG_CANDIDATES) break;
         lg_wave_sync();
     }
     __syncthreads();
@@ -592,9 +601,9 @@ __device__ __forceinline__ int lg_candidates(TopLds& lds, const LgChunk<XT, NV>&
 }
 
 template <typename XT, int NV, bool ENT, bool TOP>
-__global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80))) void logprobs_kernel(LogprobsArgs a) {
+__global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80), amdgpu_waves_per_eu(NV <= 8 ? 7 : 4))) void logprobs_kernel(LogprobsArgs a) {
     __shared__ Part parts[16];
-    __shared__ TopLds top;
+    __shared__ TopLds<NV> top;
     const int64_t t = a.row0 + blockIdx.x / (uint32_t)a.splits;
     const int chunk_number = (int)(blockIdx.x % (uint32_t)a.splits);
     const int tid = threadIdx.x, wave = tid >> 6, waves = blockDim.x >> 6;
@@ -645,7 +654,7 @@ __global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80))
 // Joins the chunks of a row: one workgroup per row
 template <typename XT, bool ENT, bool TOP>
 __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobsArgs a) {
-    __shared__ alignas(16) uint64_t list[TOP ? LG_JOIN_CANDIDATES + 2 : 1];
+    __shared__ alignas(16) uint64_t list[TOP ? LG_JOIN_CANDIDATES + 8 : 1];
     __shared__ int count;
     const int64_t t = a.row0 + blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -1090,20 +1099,32 @@ struct Plan {
 
 int vector_entries(int dtype) { return dtype == BCQ_BF16 ? 8 : 4; }
 
-// For the forward passes, with `most` threads of a workgroup for the entries.  Rows are cut where they do not fit a workgroup's registers, and where there are too few.
+// For the forward passes, with `most` threads of a workgroup for the entries.  Rows are cut where they do not fit a
+// workgroup's registers, and
+//   where fewer than 64 are there, to spread them over the card, unless alternatives are wanted, whose lists would have
+//   to be joined (us, one row of 50257 bf16, in 1 / 8 parts: without alternatives 5.2 / 4.2, with 100 12.7 / 14);
+//   where many are there and alternatives are wanted, so that more workgroups of fewer waves share a compute unit and
+//   one's search runs under another's loads (2048 rows of 50257 fp32, in 1 / 4 parts: with 20 107 / 84, with 64 132 /
+//   114, with 100 148 / 141; 4096 rows of bf16, in 1 / 2: with 20 123 / 107, with 64 148 / 152).
 Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most) {
+    constexpr int64_t kSmall = 7 * 64 * 8;  // vectors of a workgroup of seven waves
     const int64_t vectors = (V + vector_entries(dtype) - 1) / vector_entries(dtype);
     const int64_t least = (vectors + bcq::LG_MAX_NV * most - 1) / (bcq::LG_MAX_NV * most);
-    int64_t splits = (512 + T - 1) / (T > 0 ? T : 1);
+    const bool one = least == 1 && (T >= 64 || k > 0);
+    int64_t splits = one ? 1 : (512 + T - 1) / (T > 0 ? T : 1);
     const int64_t useful = (vectors + 511) / 512;
     if (splits > useful) splits = useful;
+    if (k > 0 && T >= 512) {
+        if (vectors > 8 * most) splits = (vectors + (k <= 64 ? kSmall : 8 * most) - 1) / (k <= 64 ? kSmall : 8 * most);
+        else if (k <= 32 && T >= 2048) splits = (vectors + kSmall - 1) / kSmall;
+    }
     if (splits > bcq::LG_MAX_SPLITS) splits = bcq::LG_MAX_SPLITS;
     if (k > 0 && splits * k > bcq::LG_JOIN_CANDIDATES) splits = bcq::LG_JOIN_CANDIDATES / k;
     if (splits < least) splits = least;
     Plan p;
     p.per = (int)((vectors + splits - 1) / splits);
     p.splits = (int)((vectors + p.per - 1) / p.per);
-    p.nv = p.per <= 2 * most ? 2 : p.per <= 8 * most ? 8 : 16;
+    p.nv = p.per <= 2 * most && T * p.splits <= 512 ? 2 : p.per <= 8 * most ? 8 : 16;
     p.threads = ((p.per + p.nv - 1) / p.nv + 63) / 64 * 64;
     if (p.threads < 256) p.threads = 256;
     return p;
