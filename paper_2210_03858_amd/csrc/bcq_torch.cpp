@@ -452,11 +452,12 @@ struct TokenLogprobsNode : public torch::autograd::Function<TokenLogprobsNode> {
 
 struct DistillLossNode : public torch::autograd::Function<DistillLossNode> {
     static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& logits, const Tensor& top_logit, const Tensor& top_index,
-                          const Tensor& teacher_lse, double temperature) {
+                          const OptTensor& teacher, double temperature) {
+        const Tensor teacher_lse = teacher.value_or(Tensor());
         const Table a = table(logits);
         int64_t k = 0;
         Tensor ws;
-        if (!a.ok || !list_ok(a, top_logit, top_index, teacher_lse.defined() ? OptTensor(teacher_lse) : OptTensor(), &k) ||
+        if (!a.ok || !list_ok(a, top_logit, top_index, teacher, &k) ||
             !logits_scratch(BCQ_OP_DISTILL_FWD, a, k, logits, &ws))
             throw Refused{};
         const auto options = logits.options().dtype(at::kFloat).requires_grad(false);
@@ -509,7 +510,7 @@ py::object distill_loss(const Tensor& logits, const Tensor& top_logit, const Ten
         Tensor loss;
         {
             py::gil_scoped_release release;
-            loss = DistillLossNode::apply(logits, top_logit, top_index, teacher_lse.value_or(Tensor()), temperature);
+            loss = DistillLossNode::apply(logits, top_logit, top_index, teacher_lse, temperature);
         }
         return py::cast(loss);
     } catch (const Refused&) {

@@ -416,6 +416,36 @@ def test_autograd(dtype):
         torch.autograd.grad(autograd.token_logprobs(x, tok)[0].sum(), x, create_graph=True)[0].sum().backward()
 
 
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("rest", [True, False])
+def test_autograd_nodes_agree_with_the_calls(rest, native, monkeypatch):
+    """The native nodes and the Python ones, on a table and on a batch, are the calls with the same statistics."""
+    if not native:
+        monkeypatch.setattr(bcq.binding, "_native", False)
+    T, V, k, tau = 6, 3001, 5, 1.5
+    x = table(T, V, "bf16").requires_grad_(True)
+    z, j, lse = (t.cuda() for t in teacher(x.detach(), k, tau))
+    lse = lse if rest else None
+    w = torch.rand((T,), generator=torch.Generator().manual_seed(2)).cuda()
+    loss = autograd.distill_loss(x, z, j, lse, temperature=tau)
+    dx, = torch.autograd.grad(loss, x, w)
+    stats = torch.empty((T, 4), device="cuda")
+    assert torch.equal(loss, bcq.bcq_distill_fwd(x.detach(), z, j, lse, temperature=tau, stats=stats))
+    assert torch.equal(dx, bcq.bcq_distill_bwd(x.detach(), z, j, stats, w, lse, temperature=tau))
+    cube = x.detach().reshape(2, 3, V).requires_grad_(True)
+    shape = (2, 3, k)
+    loss3 = autograd.distill_loss(cube, z.reshape(shape), j.reshape(shape), None if lse is None else lse.reshape(2, 3), temperature=tau)
+    assert torch.equal(loss3.reshape(T), loss)
+    assert torch.equal(torch.autograd.grad(loss3, cube, w.reshape(2, 3))[0].reshape(T, V), dx)
+    tok = tokens_for(T, V).cuda()
+    for entropy in (False, True):
+        out = bcq.bcq_logprobs_fwd(x.detach(), tok, temperature=tau, entropy=entropy, stats=True)
+        logp, H = autograd.token_logprobs(x, tok, temperature=tau, entropy=entropy)
+        assert torch.equal(logp, out.logp) and (torch.equal(H, out.entropy) if entropy else H is None)
+        got, = torch.autograd.grad((logp, H) if entropy else (logp,), x, (w, -w) if entropy else (w,))
+        assert torch.equal(got, bcq.bcq_logprobs_bwd(x.detach(), out.stats, tok, w, out.entropy, -w if entropy else None, temperature=tau))
+
+
 def test_gradients_against_differences():
     """Central differences of the kernels' own values along random directions.  The step is 2^-6: the values' error 2^-18 (1 + 8)
     over it is below 3e-3, the third-order term below step^2 |u|^3 <= 2.5e-4 * 30."""
