@@ -412,7 +412,6 @@ struct TopLds {
     alignas(16) float max[LG_MAX_THREADS];  // of every thread
     alignas(16) uint64_t list[LG_CANDIDATES + 8];
     uint4 words[16 * LG_SLOTS * NV];          // some threads' entries, for every wave
-    int from[16][LG_SLOTS];                  // which threads
     uint32_t counts[2][16];
     uint32_t low, high;          // keys: k entries reach `low`, none reaches `high`
     int n;
@@ -486,51 +485,50 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV>& lds, const LgChunk<XT, 
     }
     // A wave takes its few threads that hold candidates some at a time: these lay their entries out, and all lanes look at one
     // entry after another.
-    constexpr int N = LgVec<XT>::N, EACH = NV * N, ALL = LG_SLOTS * EACH;
-    constexpr int TURNS = ALL >= 64 * 2 ? 2 : (ALL + 63) / 64;  // entries of a lane at a time
+    constexpr int N = LgVec<XT>::N, EACH = NV * N, TURNS = (LG_SLOTS * EACH + 63) / 64;
     uint4* words = lds.words + wave * LG_SLOTS * NV;
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     for (uint64_t left = __ballot(tm >= bound); left;) {
+        uint64_t rest = left;
+        auto next = [&]() {
+            const int thread = rest ? __builtin_ctzll(rest) : -1;
+            rest &= rest - 1;
+            return thread;
+        };
+        const int from0 = next(), from1 = next(), from2 = next(), from3 = next();  // LG_SLOTS threads
         const int slot = __popcll(left & below);
-        const bool mine = ((left >> lane) & 1) && slot < LG_SLOTS;
-        if (mine) {
-            lds.from[wave][slot] = lane;
+        if (((left >> lane) & 1) && slot < LG_SLOTS)
 #pragma unroll
             for (int i = 0; i < NV; ++i) words[slot * NV + i] = make_uint4(chunk.w[i][0], chunk.w[i][1], chunk.w[i][2], chunk.w[i][3]);
-        }
-        const uint64_t taken = __ballot(mine);
-        const int entries = __popcll(taken) * EACH;
-        left &= ~taken;
+        left = rest;
         lg_wave_sync();
+        float x[TURNS];
+#pragma unroll
+        for (int u = 0; u < TURNS; ++u)
+            x[u] = u * 64 + lane < LG_SLOTS * EACH ? Elem<XT>::load(reinterpret_cast<const XT*>(words) + u * 64 + lane) : NAN;
+        auto place = [&](int u) {  // of this lane's entry of turn u in the chunk, past its end where there is none
+            const int e = u * 64 + lane, of = EACH < 64 ? e / EACH : u * 64 / EACH;
+            const int thread = of == 0 ? from0 : of == 1 ? from1 : of == 2 ? from2 : of == 3 ? from3 : -1;
+            return thread < 0 ? INT_MAX : e % EACH / N * chunk.threads + wave * 64 + thread;
+        };
+        uint64_t found[TURNS];
+        int total = 0;
+#pragma unroll
+        for (int u = 0; u < TURNS; ++u) {
+            found[u] = __ballot(x[u] >= bound && place(u) < chunk.n);
+            total += __popcll(found[u]);
+        }
         int at = 0;
-#pragma unroll 1
-        for (int e0 = 0; e0 < entries; e0 += 64 * TURNS) {
-            auto place = [&](int e) { return e % EACH / N * chunk.threads + wave * 64 + lds.from[wave][e / EACH]; };
-            float x[TURNS];
-            uint64_t found[TURNS];
-            int total = 0;
+        if (lane == 0) at = atomicAdd(&lds.n, total);
+        at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-            for (int u = 0; u < TURNS; ++u) {
-                const int e = e0 + u * 64 + lane;
-                x[u] = e < entries && place(e) < chunk.n ? Elem<XT>::load(reinterpret_cast<const XT*>(words) + e) : NAN;
-            }
-#pragma unroll
-            for (int u = 0; u < TURNS; ++u) {
-                found[u] = __ballot(x[u] >= bound);
-                total += __popcll(found[u]);
-            }
-            if (lane == 0) at = atomicAdd(&lds.n, total);
-            at = __builtin_amdgcn_readfirstlane(at);
-#pragma unroll
-            for (int u = 0; u < TURNS; ++u) {
-                const int here = at + __popcll(found[u] & below);
-                if (((found[u] >> lane) & 1) && here < LG_CANDIDATES)
-                    lds.list[here] = lg_entry(x[u], chunk.head + (chunk.first + place(e0 + u * 64 + lane)) * N + lane % N);
-                at += __popcll(found[u]);
-            }
+        for (int u = 0; u < TURNS; ++u) {
+            const int here = at + __popcll(found[u] & below);
+            if (((found[u] >> lane) & 1) && here < LG_CANDIDATES)
+                lds.list[here] = lg_entry(x[u], chunk.head + (chunk.first + place(u)) * N + lane % N);
+            at += __popcll(found[u]);
         }
         if (at > LG_CANDIDATES) break;
-        lg_wave_sync();
     }
     __syncthreads();
     int n = lds.n;
