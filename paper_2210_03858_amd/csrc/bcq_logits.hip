@@ -1122,7 +1122,13 @@ Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most) {
     Plan p;
     p.per = (int)((vectors + splits - 1) / splits);
     p.splits = (int)((vectors + p.per - 1) / p.per);
-    p.nv = p.per <= 2 * most && T * p.splits <= 512 ? 2 : p.per <= 8 * most ? 8 : 16;
+    // few workgroups: as many threads as there may be; many: four vectors a thread for small rows, else eight (us, with 20
+    // alternatives, at 2 / 4 / 8: 200 rows of 8192 bf16 5.9 / 6.7 / 8.2, 16384 of them 95 / 65 / 81, 4571 rows of 18610 at 4 / 8
+    // 61 / 43)
+    const bool few = T * p.splits <= 512;
+    if (few && p.per <= 2 * most) p.nv = 2;
+    else if (p.per <= (few ? 4 * most : 1536)) p.nv = 4;
+    else p.nv = p.per <= 8 * most ? 8 : 16;
     p.threads = ((p.per + p.nv - 1) / p.nv + 63) / 64 * 64;
     if (p.threads < 256) p.threads = 256;
     return p;
@@ -1167,6 +1173,7 @@ void launch_logprobs_nv(const bcq::LogprobsArgs& a, int64_t T, int threads, hipS
 template <typename XT>
 hipError_t launch_logprobs(const bcq::LogprobsArgs& a, int64_t T, const Plan& p, hipStream_t st) {
     if (p.nv == 2) launch_logprobs_nv<XT, 2>(a, T, p.threads, st);
+    else if (p.nv == 4) launch_logprobs_nv<XT, 4>(a, T, p.threads, st);
     else if (p.nv == 8) launch_logprobs_nv<XT, 8>(a, T, p.threads, st);
     else launch_logprobs_nv<XT, 16>(a, T, p.threads, st);
     return hipGetLastError();
@@ -1190,12 +1197,17 @@ void launch_distill_as(bcq::DistillArgs a, int64_t T, int threads, hipStream_t s
         if (MODE == bcq::LG_SUMS) BCQ_LAUNCH((bcq::distill_join_kernel<XT, REST>), dim3(rows), dim3(64), 0, st, a);
     });
 }
+template <typename XT, int NV, bcq::DistillMode MODE>
+void launch_distill_nv(const bcq::DistillArgs& a, int64_t T, int threads, hipStream_t st) {
+    if (a.teacher_lse) launch_distill_as<XT, NV, true, MODE>(a, T, threads, st);
+    else launch_distill_as<XT, NV, false, MODE>(a, T, threads, st);
+}
 template <typename XT, bcq::DistillMode MODE>
 hipError_t launch_distill(const bcq::DistillArgs& a, int64_t T, const Plan& p, hipStream_t st) {
-    const bool rest = a.teacher_lse != nullptr;
-    if (p.nv == 2) rest ? launch_distill_as<XT, 2, true, MODE>(a, T, p.threads, st) : launch_distill_as<XT, 2, false, MODE>(a, T, p.threads, st);
-    else if (p.nv == 8) rest ? launch_distill_as<XT, 8, true, MODE>(a, T, p.threads, st) : launch_distill_as<XT, 8, false, MODE>(a, T, p.threads, st);
-    else rest ? launch_distill_as<XT, 16, true, MODE>(a, T, p.threads, st) : launch_distill_as<XT, 16, false, MODE>(a, T, p.threads, st);
+    if (p.nv == 2) launch_distill_nv<XT, 2, MODE>(a, T, p.threads, st);
+    else if (p.nv == 4) launch_distill_nv<XT, 4, MODE>(a, T, p.threads, st);
+    else if (p.nv == 8) launch_distill_nv<XT, 8, MODE>(a, T, p.threads, st);
+    else launch_distill_nv<XT, 16, MODE>(a, T, p.threads, st);
     return hipGetLastError();
 }
 template <typename XT>
