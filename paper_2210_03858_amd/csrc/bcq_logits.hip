@@ -1043,7 +1043,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a) {
 
 template <typename XT, int NV, bool REST>
 __global__ __launch_bounds__(256) void distill_bwd_kernel(DistillArgs a) {
-    __shared__ int index[BCQ_LOGITS_MAX_K];
+    __shared__ alignas(16) int index[BCQ_LOGITS_MAX_K];
     __shared__ float prob[BCQ_LOGITS_MAX_K];
     const int64_t t = a.row0 + blockIdx.x / (uint32_t)a.splits;
     const int chunk_number = (int)(blockIdx.x % (uint32_t)a.splits);
@@ -1070,7 +1070,7 @@ __global__ __launch_bounds__(256) void distill_bwd_kernel(DistillArgs a) {
         const double norm = REST ? a.teacher_lse[t] : stats[2];
         p = lg_exp2((float)(((double)a.top_logit[t * a.k + tid] * a.c - norm) * M_LOG2E));
     }
-    if (tid < a.k) {
+    if (tid < BCQ_LOGITS_MAX_K) {
         index[tid] = listed;
         prob[tid] = p;
     }
@@ -1078,9 +1078,17 @@ __global__ __launch_bounds__(256) void distill_bwd_kernel(DistillArgs a) {
     const float f = w * d.f;
     if (f == 0.f) chunk.store(drow, [&](float) { return 0.f; });
     else chunk.store(drow, [&](float v) { return f * lg_exp2((v - d.m) * c2); });
-    if (mine)  // an index that stands more than once has all its entries' probability
-        for (int i = 0; i < a.k; ++i)
-            if (index[i] == listed && i != tid) p += prob[i];
+    if (mine) {  // an index that stands more than once has all its entries' probability
+        p = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < a.k; i += 4) {
+            const int4 four = *reinterpret_cast<const int4*>(index + i);
+            if (four.x == listed) p += prob[i];
+            if (four.y == listed) p += prob[i + 1];
+            if (four.z == listed) p += prob[i + 2];
+            if (four.w == listed) p += prob[i + 3];
+        }
+    }
     __syncthreads();
     if (mine) Elem<XT>::store(drow + listed, lg_listed_gradient(d, s, p, a.c, w));
 }
@@ -1101,20 +1109,23 @@ int vector_entries(int dtype) { return dtype == BCQ_BF16 ? 8 : 4; }
 // workgroup's registers, and
 //   where fewer than 64 are there, to spread them over the card, unless alternatives are wanted, whose lists would have
 //   to be joined (us, one row of 50257 bf16, in 1 / 8 parts: without alternatives 5.2 / 4.2, with 100 12.7 / 14);
-//   where many are there and alternatives are wanted, so that more workgroups of fewer waves share a compute unit and
-//   one's search runs under another's loads (2048 rows of 50257 fp32, in 1 / 4 parts: with 20 107 / 84, with 64 132 /
-//   114, with 100 148 / 141; 4096 rows of bf16, in 1 / 2: with 20 123 / 107, with 64 148 / 152).
-Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most) {
+//   where alternatives are wanted of many or of long rows, so that more workgroups of fewer waves share a compute unit
+//   and one's search runs under another's loads (2048 rows of 50257 fp32, in 1 / 4 parts: with 20 105 / 84, with 64 127 /
+//   114, with 100 142 / 140; 4096 rows of bf16, in 1 / 2: with 20 121 / 102, with 64 140 / 140; 200 rows of 250007 bf16, in
+//   2 / 8: with 20 37 / 28, in 2 / 4: with 100 47 / 41).
+// The distillation's list is read in every workgroup of a row that is not cut, and in a launch of its own where it is: rows that
+// fit eight vectors a thread are not (loss and gradient of 24 rows of 50257 bf16, in 1 / 8 parts 9.2 / 11).
+Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most, bool listed) {
     constexpr int64_t kSmall = 7 * 64 * 8;  // vectors of a workgroup of seven waves
     const int64_t vectors = (V + vector_entries(dtype) - 1) / vector_entries(dtype);
     const int64_t least = (vectors + bcq::LG_MAX_NV * most - 1) / (bcq::LG_MAX_NV * most);
-    const bool one = least == 1 && (T >= 64 || k > 0);
+    const bool one = least == 1 && (T >= 64 || k > 0 || (listed && vectors <= 8 * most));
     int64_t splits = one ? 1 : (512 + T - 1) / (T > 0 ? T : 1);
     const int64_t useful = (vectors + 511) / 512;
     if (splits > useful) splits = useful;
-    if (k > 0 && T >= 512) {
-        if (vectors > 8 * most) splits = (vectors + (k <= 64 ? kSmall : 8 * most) - 1) / (k <= 64 ? kSmall : 8 * most);
-        else if (k <= 32 && T >= 2048) splits = (vectors + kSmall - 1) / kSmall;
+    if (k > 0 && (least > 1 || (T >= 512 && vectors > 8 * most) || (T >= 2048 && k <= 32))) {
+        const int64_t part = k <= 64 ? kSmall : 8 * most;
+        splits = (vectors + part - 1) / part;
     }
     if (splits > bcq::LG_MAX_SPLITS) splits = bcq::LG_MAX_SPLITS;
     if (k > 0 && splits * k > bcq::LG_JOIN_CANDIDATES) splits = bcq::LG_JOIN_CANDIDATES / k;
@@ -1133,8 +1144,8 @@ Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most) {
     if (p.threads < 256) p.threads = 256;
     return p;
 }
-Plan logprobs_plan(int64_t T, int64_t V, int dtype, int k) { return forward_plan(T, V, dtype, k, bcq::LG_MAX_THREADS); }
-Plan distill_plan(int64_t T, int64_t V, int dtype) { return forward_plan(T, V, dtype, 0, bcq::LG_MAX_THREADS - 64); }
+Plan logprobs_plan(int64_t T, int64_t V, int dtype, int k) { return forward_plan(T, V, dtype, k, bcq::LG_MAX_THREADS, false); }
+Plan distill_plan(int64_t T, int64_t V, int dtype) { return forward_plan(T, V, dtype, 0, bcq::LG_MAX_THREADS - 64, true); }
 // For the gradients from saved statistics: nothing is joined, so chunks are small.
 constexpr int kBwdNv = 4;
 Plan backward_plan(int64_t V, int dtype) {
