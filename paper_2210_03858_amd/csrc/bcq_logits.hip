@@ -278,22 +278,25 @@ struct LgChunk {
         p.S += S2;
         reread();
         if (!(p.S < 0x1p32f && p.S > 0x1p-32f)) {
-            top = max();
+            if (!MAX) top = max();
+            const bool nothing = p.S == 0.f && top == -INFINITY;  // masks only; NaN alone have a sum
             p = Part{top, 0.f, 0.f};
             m = lg_shift(top);
-            add((edge - m) * c2, p.S);
+            if (!nothing) {
+                add((edge - m) * c2, p.S);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (any(i)) {
-                    uint32_t v[4];
+                for (int i = 0; i < NV; ++i)
+                    if (any(i)) {
+                        uint32_t v[4];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        v[u] = w[i][u];
-                        asm volatile("" : "+v"(v[u]));
+                        for (int u = 0; u < 4; ++u) {
+                            v[u] = w[i][u];
+                            asm volatile("" : "+v"(v[u]));
+                        }
+#pragma unroll
+                        for (int e = 0; e < Vec::N; ++e) add((Vec::get(v, e) - m) * c2, p.S);
                     }
-#pragma unroll
-                    for (int e = 0; e < Vec::N; ++e) add((Vec::get(v, e) - m) * c2, p.S);
-                }
+            }
         }
         return p;
     }
@@ -478,6 +481,10 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV>& lds, const LgChunk<XT, 
     if (wave == 0) lg_bound(lds, k);
     __syncthreads();
     uint32_t low = lds.low, high = lds.high;
+    // A bound as low as a mask's value: the masked entries are many, so only those above are taken, and as many of the masked
+    // as are missing then looked for in order.
+    const bool masks = lg_unkey(low) < -0x1p100f;
+    if (masks) ++low;
     const float bound = lg_unkey(low);
     if (chunk.edge_index >= 0 && chunk.edge >= bound) {
         const int at = atomicAdd(&lds.n, 1);
@@ -532,47 +539,49 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV>& lds, const LgChunk<XT, 
     }
     __syncthreads();
     int n = lds.n;
-    if (n <= LG_CANDIDATES) return n;
-
-    // Too many: equal entries in great number, as masks leave them, or large entries that meet in few threads.
-    __syncthreads();
-    int turn = 0;
-    auto above = [&](float at) {  // number of entries above a value
-        uint32_t c = 0;
-        chunk.scan(row, [&](float x, int) { c += x > at ? 1u : 0u; });
-        c = wave_sum(c);
-        turn ^= 1;  // the counts of the last call may still be read
-        if (lane == 0) lds.counts[turn][threadIdx.x >> 6] = c;
+    float value;  // n entries are above it, fewer than k; the others equal it
+    if (n <= LG_CANDIDATES) {
+        if (!masks || n >= k) return n;
+        value = lg_unkey(low - 1);
+    } else {
+        // Too many: equal entries in great number, or large entries that meet in few threads.
         __syncthreads();
-        int total = 0;
-        for (int v = 0; v < waves; ++v) total += (int)lds.counts[turn][v];
-        return total;
-    };
-    // where the entries above the bound are still too many, it is moved to the k-th value by halving
-    int greater = above(lg_unkey(low));
-    if (greater > LG_CANDIDATES) {
-        while (high - low > 1) {  // k or more exceed `low`, fewer than k exceed `high`
-            const uint32_t mid = low + (high - low) / 2;
-            if (above(lg_unkey(mid)) >= k) low = mid;
-            else high = mid;
+        int turn = 0;
+        auto above = [&](float at) {  // number of entries above a value
+            uint32_t c = 0;
+            chunk.scan(row, [&](float x, int) { c += x > at ? 1u : 0u; });
+            c = wave_sum(c);
+            turn ^= 1;  // the counts of the last call may still be read
+            if (lane == 0) lds.counts[turn][wave] = c;
+            __syncthreads();
+            int total = 0;
+            for (int v = 0; v < waves; ++v) total += (int)lds.counts[turn][v];
+            return total;
+        };
+        // where the entries above the bound are still too many, it is moved to the k-th value by halving
+        n = above(bound);
+        if (n > LG_CANDIDATES) {
+            while (high - low > 1) {  // k or more exceed `low`, fewer than k exceed `high`
+                const uint32_t mid = low + (high - low) / 2;
+                if (above(lg_unkey(mid)) >= k) low = mid;
+                else high = mid;
+            }
+            low = high;
+            n = above(lg_unkey(low));
         }
-        low = high;
-        greater = above(lg_unkey(low));
+        value = lg_unkey(low);
+        if (threadIdx.x == 0) lds.n = 0;
+        __syncthreads();
+        chunk.scan(row, [&](float x, int index) {
+            if (x > value) lds.list[atomicAdd(&lds.n, 1)] = lg_entry(x, index);
+        });
+        __syncthreads();
+        if (n >= k) return n;
     }
-    const float value = lg_unkey(low);
-    if (threadIdx.x == 0) lds.n = 0;
-    __syncthreads();
-    chunk.scan(row, [&](float x, int index) {
-        if (x > value) lds.list[atomicAdd(&lds.n, 1)] = lg_entry(x, index);
-    });
-    __syncthreads();
-    n = greater;
-    if (n >= k) return n;
-    // the others equal the bound: the first of them by column, which the first wave looks for in order
-    if (threadIdx.x < 64) {
-        const int begin = chunk.first == 0 ? 0 : chunk.head + chunk.first * LgVec<XT>::N;
-        const int end = chunk.head + (chunk.first + chunk.n) * LgVec<XT>::N;
-        const int tail = chunk.head + (V - chunk.head) / LgVec<XT>::N * LgVec<XT>::N;
+    // the first of the equal entries by column, which the first wave looks for in order
+    if (wave == 0) {
+        const int begin = chunk.first == 0 ? 0 : chunk.head + chunk.first * N;
+        const int end = chunk.head + (chunk.first + chunk.n) * N, tail = chunk.head + chunk.vectors * N;
         int at = n;
         for (int part = 0; part < 2; ++part) {
             const int from = part ? (end > tail ? end : tail) : begin, to = part ? (chunk.first == 0 ? V : 0) : end;
@@ -586,7 +595,7 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV>& lds, const LgChunk<XT, 
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const uint64_t equal = __ballot(x[u] == value);
-                    const int mine = at + __popcll(equal & (((uint64_t)1 << lane) - 1));
+                    const int mine = at + __popcll(equal & below);
                     if (x[u] == value && mine < k) lds.list[mine] = lg_entry(value, i + u * 64 + lane);
                     at += __popcll(equal);
                 }
