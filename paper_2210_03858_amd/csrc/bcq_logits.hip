@@ -18,6 +18,7 @@ constexpr float LG_LOG2E = 1.4426950408889634f;
 constexpr float LG_LN2 = 0.6931471805599453f;
 constexpr int LG_MAX_THREADS = 1024;
 constexpr int LG_MAX_NV = 16;          // vectors per thread at most
+constexpr int LG_MAX_NV_GRADIENT = 24;  // where loss and gradient come from one reading of the row
 constexpr int LG_MAX_SPLITS = 64;      // chunks per row at most: a wave joins them, one per lane
 constexpr int LG_CANDIDATES = 1024;    // entries that are ranked against each other
 constexpr int LG_JOIN_CANDIDATES = 2048;
@@ -1124,10 +1125,10 @@ int vector_entries(int dtype) { return dtype == BCQ_BF16 ? 8 : 4; }
 //   2 / 8: with 20 37 / 28, in 2 / 4: with 100 47 / 41).
 // The distillation's list is read in every workgroup of a row that is not cut, and in a launch of its own where it is: rows that
 // fit eight vectors a thread are not (loss and gradient of 24 rows of 50257 bf16, in 1 / 8 parts 9.2 / 11).
-Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most, bool listed) {
+Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most, int most_nv, bool listed) {
     constexpr int64_t kSmall = 7 * 64 * 8;  // vectors of a workgroup of seven waves
     const int64_t vectors = (V + vector_entries(dtype) - 1) / vector_entries(dtype);
-    const int64_t least = (vectors + bcq::LG_MAX_NV * most - 1) / (bcq::LG_MAX_NV * most);
+    const int64_t least = (vectors + most_nv * most - 1) / (most_nv * most);
     const bool one = least == 1 && (T >= 64 || k > 0 || (listed && vectors <= 8 * most));
     int64_t splits = one ? 1 : (512 + T - 1) / (T > 0 ? T : 1);
     const int64_t useful = (vectors + 511) / 512;
@@ -1148,13 +1149,19 @@ Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most, bool listed)
     const bool few = T * p.splits <= 512;
     if (few && p.per <= 2 * most) p.nv = 2;
     else if (p.per <= (few ? 4 * most : 1536)) p.nv = 4;
-    else p.nv = p.per <= 8 * most ? 8 : 16;
+    else p.nv = p.per <= 8 * most ? 8 : p.per <= 16 * most ? 16 : most_nv;
     p.threads = ((p.per + p.nv - 1) / p.nv + 63) / 64 * 64;
     if (p.threads < 256) p.threads = 256;
     return p;
 }
-Plan logprobs_plan(int64_t T, int64_t V, int dtype, int k) { return forward_plan(T, V, dtype, k, bcq::LG_MAX_THREADS, false); }
-Plan distill_plan(int64_t T, int64_t V, int dtype) { return forward_plan(T, V, dtype, 0, bcq::LG_MAX_THREADS - 64, true); }
+Plan logprobs_plan(int64_t T, int64_t V, int dtype, int k) { return forward_plan(T, V, dtype, k, bcq::LG_MAX_THREADS, bcq::LG_MAX_NV, false); }
+Plan distill_plan(int64_t T, int64_t V, int dtype, bool gradient) {
+    const int64_t vectors = (V + vector_entries(dtype) - 1) / vector_entries(dtype);
+    const int most = bcq::LG_MAX_THREADS - 64;
+    // a row of that many vectors per thread is a workgroup's only if the gradient follows (else reading it twice costs nothing)
+    const int nv = gradient && vectors <= bcq::LG_MAX_NV_GRADIENT * most ? bcq::LG_MAX_NV_GRADIENT : bcq::LG_MAX_NV;
+    return forward_plan(T, V, dtype, 0, most, nv, true);
+}
 // For the gradients from saved statistics: nothing is joined, so chunks are small.
 constexpr int kBwdNv = 4;
 Plan backward_plan(int64_t V, int dtype) {
@@ -1227,7 +1234,8 @@ hipError_t launch_distill(const bcq::DistillArgs& a, int64_t T, const Plan& p, h
     if (p.nv == 2) launch_distill_nv<XT, 2, MODE>(a, T, p.threads, st);
     else if (p.nv == 4) launch_distill_nv<XT, 4, MODE>(a, T, p.threads, st);
     else if (p.nv == 8) launch_distill_nv<XT, 8, MODE>(a, T, p.threads, st);
-    else launch_distill_nv<XT, 16, MODE>(a, T, p.threads, st);
+    else if (p.nv == 16) launch_distill_nv<XT, 16, MODE>(a, T, p.threads, st);
+    else if constexpr (MODE == bcq::LG_GRADIENT) launch_distill_nv<XT, bcq::LG_MAX_NV_GRADIENT, MODE>(a, T, p.threads, st);
     return hipGetLastError();
 }
 template <typename XT>
@@ -1263,7 +1271,7 @@ bcq_status done(hipError_t e) { return e == hipSuccess ? BCQ_OK : BCQ_ERR_DEVICE
 // The partial sums of split rows (16 bytes a chunk), then their lists of alternatives, or the statistics between a loss
 // and its gradient (16 bytes a row).
 size_t workspace_need(int op, int64_t T, int64_t V, int k, int dtype) {
-    const Plan p = op == BCQ_OP_LOGPROBS_FWD ? logprobs_plan(T, V, dtype, k) : distill_plan(T, V, dtype);
+    const Plan p = op == BCQ_OP_LOGPROBS_FWD ? logprobs_plan(T, V, dtype, k) : distill_plan(T, V, dtype, op == BCQ_OP_DISTILL_FWD_BWD);
     if (p.splits == 1) return 0;
     const size_t parts = (size_t)T * p.splits * 16;
     if (op == BCQ_OP_LOGPROBS_FWD) return parts + (size_t)T * p.splits * k * 8;
@@ -1404,7 +1412,7 @@ bcq_status bcq_distill_fwd(const void* logits, int dtype, int64_t T, int64_t V, 
     if (w != BCQ_OK) return w;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    const Plan p = distill_plan(T, V, dtype);
+    const Plan p = distill_plan(T, V, dtype, false);
     bcq::DistillArgs d = distill_args(a);
     d.loss = loss;
     d.stats = stats;
@@ -1450,7 +1458,7 @@ bcq_status bcq_distill_fwd_bwd(const void* logits, int dtype, int64_t T, int64_t
     if (s != BCQ_OK) return s;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    const Plan p = distill_plan(T, V, dtype);
+    const Plan p = distill_plan(T, V, dtype, true);
     bcq::DistillArgs d = distill_args(a);
     d.weight = weight;
     d.loss = loss;

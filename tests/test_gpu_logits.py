@@ -92,7 +92,7 @@ def close_grad(got, ref, terms):
 SHAPES = [  # T, V, stride, offset
     (1, 1, None, 0), (3, 2, None, 0), (1, 7, None, 0), (2, 8, None, 0), (5, 31, 33, 1), (3, 130, None, 3), (300, 257, None, 0),
     (4, 1000, 1003, 5), (7, 4099, None, 0), (2, 32003, 32064, 0), (1, 50257, None, 0), (6, 50257, None, 7),
-    (1100, 5003, None, 0), (520, 33001, None, 1), (2, 65537, None, 0), (3, 131075, 131077, 0), (1, 250007, None, 0), (300, 140001, None, 0),
+    (1100, 5003, None, 0), (520, 33001, None, 1), (2, 65537, None, 0), (3, 131075, 131077, 0), (1, 250007, None, 0), (300, 140001, None, 0), (70, 70001, 70003, 2),
 ]
 
 
