@@ -17,6 +17,7 @@ namespace bcq {
 constexpr float LG_LOG2E = 1.4426950408889634f;
 constexpr float LG_LN2 = 0.6931471805599453f;
 constexpr int LG_MAX_THREADS = 1024;
+constexpr int LG_QUARTERS = LG_MAX_THREADS / 4;
 constexpr int LG_MAX_NV = 16;               // vectors per thread at most
 constexpr int LG_MAX_NV_GRADIENT = 24;      // where loss and gradient come from one reading of the row
 constexpr int LG_MAX_SPLITS = 64;           // chunks per row at most: a wave joins them, one per lane
@@ -228,6 +229,16 @@ struct LgChunk {
                 for (int e = 0; e < Vec::N; e += 2) m = lg_max3(m, Vec::get(w[i], e), Vec::get(w[i], e + 1));
         return lg_max2(m, -INFINITY);
     }
+    // The thread's maxima over every fourth entry, for rows so short that the threads' own are too few to bound anything
+    __device__ __forceinline__ float4 quarters() const {
+        float m[4] = {edge, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (any(i))
+#pragma unroll
+                for (int e = 0; e < Vec::N; ++e) m[e & 3] = lg_max2(m[e & 3], Vec::get(w[i], e));
+        return make_float4(lg_max2(m[0], -INFINITY), m[1], m[2], m[3]);
+    }
     // NaN made quiet: the maximum instructions leave those out and take a signalling one for the result
     __device__ __forceinline__ void quiet() {
         if (edge != edge) edge = NAN;
@@ -410,26 +421,30 @@ __device__ __forceinline__ void lg_rank(uint64_t* list, int n, int k, F put) {
     for (int r = n + (int)threadIdx.x; r < k; r += blockDim.x) put(r, (uint64_t)0);
 }
 
-template <int NV>
+// How a wave of logprobs_kernel finds its candidates for the alternatives: LG_STAGED, the entries of the few threads that
+// hold some by all lanes together; LG_DIRECT, every thread its own, one place of its registers after another.
+enum LogprobsTop { LG_NO_TOP, LG_STAGED, LG_DIRECT };
+template <int NV, LogprobsTop TOP>
 struct TopLds {
-    alignas(16) float max[LG_MAX_THREADS];  // of every thread
+    alignas(16) float max[LG_MAX_THREADS];  // of every thread, four of each in workgroups of at most LG_QUARTERS threads
     alignas(16) uint64_t list[LG_CANDIDATES + 8];
-    uint4 words[16 * LG_SLOTS * NV];          // some threads' entries, for every wave
+    uint4 words[TOP == LG_STAGED ? 16 * LG_SLOTS * NV : 1];  // some threads' entries, for every wave
     uint32_t counts[2][16];
     uint32_t low, high;          // keys: k entries reach `low`, none reaches `high`
     int n;
 };
 
-// The search for the candidates' bound, by one wave.  The threads are cut into 64 R groups, R the least power of two with
+// The search for the candidates' bound, by one wave.  The maxima are cut into 64 R groups, R the least power of two with
 // 32 R >= k.  At least k groups have a maximum that reaches the k-th largest of the groups' maxima, so that value is a lower
 // bound of the k-th entry, and few entries exceed it: with entries in random order -64 R ln(1 - k / (64 R)), 24 for the 20
 // best, 89 for 64.  The bound only has to be low enough, so its search by halving stops early, at 26 and 95 entries in the
 // mean.
-template <int NV>
-__device__ __forceinline__ void lg_bound(TopLds<NV>& lds, int k) {
+template <typename L>
+__device__ __forceinline__ void lg_bound(L& lds, int k) {
     const int lane = threadIdx.x & 63;
     float group[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    for (int i = lane; i < (int)blockDim.x / 4; i += 64) {
+    const int fours = (int)blockDim.x <= LG_QUARTERS ? (int)blockDim.x : (int)blockDim.x / 4;
+    for (int i = lane; i < fours; i += 64) {
         const float4 q = reinterpret_cast<const float4*>(lds.max)[i];
         group[0] = lg_max2(group[0], q.x);
         group[1] = lg_max2(group[1], q.y);
@@ -476,8 +491,8 @@ __device__ __forceinline__ void lg_bound(TopLds<NV>& lds, int k) {
 
 // The candidates for a chunk's k best in lds.list, and their number.  Called by all threads after lds.max is written and a
 // barrier.
-template <typename XT, int NV>
-__device__ __forceinline__ int lg_candidates(TopLds<NV>& lds, const LgChunk<XT, NV>& chunk, const XT* row, int V, float tm, int k) {
+template <typename XT, int NV, LogprobsTop TOP>
+__device__ __forceinline__ int lg_candidates(TopLds<NV, TOP>& lds, LgChunk<XT, NV>& chunk, const XT* row, int V, float tm, int k) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     if (wave == 0) lg_bound(lds, k);
     __syncthreads();
@@ -491,52 +506,83 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV>& lds, const LgChunk<XT, 
         const int at = atomicAdd(&lds.n, 1);
         if (at < LG_CANDIDATES) lds.list[at] = lg_entry(chunk.edge, chunk.edge_index);
     }
-    // A wave takes its few threads that hold candidates some at a time: these lay their entries out, and all lanes look at one
-    // entry after another.
     constexpr int N = LgVec<XT>::N, EACH = NV * N, TURNS = (LG_SLOTS * EACH + 63) / 64;
-    uint4* words = lds.words + wave * LG_SLOTS * NV;
     const uint64_t below = ((uint64_t)1 << lane) - 1;
-    for (uint64_t left = __ballot(tm >= bound); left;) {
-        uint64_t rest = left;
-        auto next = [&]() {
-            const int thread = rest ? __builtin_ctzll(rest) : -1;
-            rest &= rest - 1;
-            return thread;
-        };
-        const int from0 = next(), from1 = next(), from2 = next(), from3 = next();  // LG_SLOTS threads
-        const int slot = __popcll(left & below);
-        if (((left >> lane) & 1) && slot < LG_SLOTS)
+    // The bound is above -inf: a chunk's end is none.
+    const uint64_t holders = __ballot(tm >= bound);
+    if (TOP == LG_DIRECT && holders) {  // counts its candidates, takes as many places of the list at once and fills them
+        int found[NV], total = 0;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) words[slot * NV + i] = make_uint4(chunk.w[i][0], chunk.w[i][1], chunk.w[i][2], chunk.w[i][3]);
-        left = rest;
-        lg_wave_sync();
-        float x[TURNS];
+        for (int i = 0; i < NV; ++i) {
+            found[i] = 0;
+            if (chunk.any(i))
 #pragma unroll
-        for (int u = 0; u < TURNS; ++u)
-            x[u] = u * 64 + lane < LG_SLOTS * EACH ? Elem<XT>::load(reinterpret_cast<const XT*>(words) + u * 64 + lane) : NAN;
-        auto place = [&](int u) {  // of this lane's entry of turn u in the chunk, past its end where there is none
-            const int e = u * 64 + lane, of = EACH < 64 ? e / EACH : u * 64 / EACH;
-            const int thread = of == 0 ? from0 : of == 1 ? from1 : of == 2 ? from2 : of == 3 ? from3 : -1;
-            return thread < 0 ? INT_MAX : e % EACH / N * chunk.threads + wave * 64 + thread;
-        };
-        uint64_t found[TURNS];
-        int total = 0;
-#pragma unroll
-        for (int u = 0; u < TURNS; ++u) {
-            found[u] = __ballot(x[u] >= bound && place(u) < chunk.n);
-            total += __popcll(found[u]);
+                for (int e = 0; e < N; ++e) found[i] += __popcll(__ballot(LgVec<XT>::get(chunk.w[i], e) >= bound));
+            total += found[i];
         }
+        chunk.reread();
         int at = 0;
         if (lane == 0) at = atomicAdd(&lds.n, total);
         at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-        for (int u = 0; u < TURNS; ++u) {
-            const int here = at + __popcll(found[u] & below);
-            if (((found[u] >> lane) & 1) && here < LG_CANDIDATES)
-                lds.list[here] = lg_entry(x[u], chunk.head + (chunk.first + place(u)) * N + lane % N);
-            at += __popcll(found[u]);
+        for (int i = 0; i < NV; ++i)
+            if (found[i] > 0)
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float x = LgVec<XT>::get(chunk.w[i], e);
+                    const uint64_t these = __ballot(x >= bound);
+                    const int here = at + __popcll(these & below);
+                    if (x >= bound && here < LG_CANDIDATES)
+                        lds.list[here] = lg_entry(x, chunk.head + (chunk.first + chunk.place_of(i)) * N + e);
+                    at += __popcll(these);
+                }
+    }
+    if constexpr (TOP == LG_STAGED) {
+        // takes the threads that hold candidates some at a time: these lay their entries out, and all lanes look at one entry
+        // after another
+        uint4* words = lds.words + wave * LG_SLOTS * NV;
+        for (uint64_t left = holders; left;) {
+            uint64_t rest = left;
+            auto next = [&]() {
+                const int thread = rest ? __builtin_ctzll(rest) : -1;
+                rest &= rest - 1;
+                return thread;
+            };
+            const int from0 = next(), from1 = next(), from2 = next(), from3 = next();  // LG_SLOTS threads
+            const int slot = __popcll(left & below);
+            if (((left >> lane) & 1) && slot < LG_SLOTS)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) words[slot * NV + i] = make_uint4(chunk.w[i][0], chunk.w[i][1], chunk.w[i][2], chunk.w[i][3]);
+            left = rest;
+            lg_wave_sync();
+            float x[TURNS];
+#pragma unroll
+            for (int u = 0; u < TURNS; ++u)
+                x[u] = u * 64 + lane < LG_SLOTS * EACH ? Elem<XT>::load(reinterpret_cast<const XT*>(words) + u * 64 + lane) : NAN;
+            auto place = [&](int u) {  // of this lane's entry of turn u in the chunk, past its end where there is none
+                const int e = u * 64 + lane, of = EACH < 64 ? e / EACH : u * 64 / EACH;
+                const int thread = of == 0 ? from0 : of == 1 ? from1 : of == 2 ? from2 : of == 3 ? from3 : -1;
+                return thread < 0 ? INT_MAX : e % EACH / N * chunk.threads + wave * 64 + thread;
+            };
+            uint64_t found[TURNS];
+            int total = 0;
+#pragma unroll
+            for (int u = 0; u < TURNS; ++u) {
+                found[u] = __ballot(x[u] >= bound && place(u) < chunk.n);
+                total += __popcll(found[u]);
+            }
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&lds.n, total);
+            at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+            for (int u = 0; u < TURNS; ++u) {
+                const int here = at + __popcll(found[u] & below);
+                if (((found[u] >> lane) & 1) && here < LG_CANDIDATES)
+                    lds.list[here] = lg_entry(x[u], chunk.head + (chunk.first + place(u)) * N + lane % N);
+                at += __popcll(found[u]);
+            }
+            if (at > LG_CANDIDATES) break;
         }
-        if (at > LG_CANDIDATES) break;
     }
     __syncthreads();
     int n = lds.n;
@@ -615,16 +661,16 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV>& lds, const LgChunk<XT, 
 // 50257 fp32 with 64 alternatives in 115 us, 3.6 TB/s.  So residency counts.  Eight waves a SIMD need at most 64 vector and
 // 80 scalar registers each (the compiler by itself takes 96 of these), which the attributes ask for; sixteen vectors a
 // thread do not fit that and get the registers of four waves.
-template <typename XT, int NV, bool ENT, bool TOP>
+template <typename XT, int NV, bool ENT, LogprobsTop TOP>
 __global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80), amdgpu_waves_per_eu(NV <= 8 ? 7 : 4))) void logprobs_kernel(LogprobsArgs a) {
     __shared__ Part parts[16];
-    __shared__ TopLds<NV> top;
+    __shared__ TopLds<NV, TOP> top;
     const int64_t t = a.row0 + blockIdx.x / (uint32_t)a.splits;
     const int chunk_number = (int)(blockIdx.x % (uint32_t)a.splits);
     const int tid = threadIdx.x, wave = tid >> 6, waves = blockDim.x >> 6;
     const float c2 = a.c * LG_LOG2E;
     const int64_t token = a.tokens ? a.tokens[t] : -1;
-    if (!ENT && !TOP && token < 0 && !a.lse) {  // nothing of this row is wanted
+    if (!ENT && TOP == LG_NO_TOP && token < 0 && !a.lse) {  // nothing of this row is wanted
         if (tid == 0 && chunk_number == 0) {
             if (a.logp) a.logp[t] = 0.f;
             if (a.stats) a.stats[2 * t] = a.stats[2 * t + 1] = 0.f;
@@ -636,12 +682,14 @@ __global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80),
     chunk.place(row, a.V, chunk_number, a.per);
     chunk.load(row, blockDim.x);
     float tm;
-    Part p = lg_wave_join<ENT>(chunk.template sums<ENT, TOP>(c2, tm), c2);
+    Part p = lg_wave_join<ENT>(chunk.template sums<ENT, TOP != LG_NO_TOP>(c2, tm), c2);
     chunk.reread();
     if ((tid & 63) == 0) parts[wave] = p;
-    if constexpr (TOP) {
-        top.max[tid] = tm;
-    }
+    auto write_max = [&]() {
+        if ((int)blockDim.x <= LG_QUARTERS) reinterpret_cast<float4*>(top.max)[tid] = chunk.quarters();
+        else top.max[tid] = tm;
+    };
+    if constexpr (TOP != LG_NO_TOP) write_max();
     __syncthreads();
     p = lg_parts_join<ENT>(parts, waves, c2);
     const bool whole = a.splits == 1;
@@ -650,14 +698,14 @@ __global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80),
         if (whole) lg_write_row<XT>(a, t, token, p, l2);
         else a.parts[t * a.splits + chunk_number] = make_float4(p.m, p.S, p.E, 0.f);
     }
-    if constexpr (TOP) {
+    if constexpr (TOP != LG_NO_TOP) {
         if (p.S != p.S) {  // the maxima may not be what they should
             chunk.quiet();
             tm = chunk.max();
-            top.max[tid] = tm;
+            write_max();
             __syncthreads();
         }
-        const int n = lg_candidates<XT, NV>(top, chunk, row, a.V, tm, a.k);
+        const int n = lg_candidates<XT, NV, TOP>(top, chunk, row, a.V, tm, a.k);
         if (whole) lg_rank(top.list, n, a.k, [&](int rank, uint64_t entry) { lg_write_top(a, t, rank, entry, p, l2); });
         else {
             uint64_t* list = a.lists + (t * a.splits + chunk_number) * a.k;
@@ -1136,7 +1184,7 @@ int vector_entries(int dtype) { return dtype == BCQ_BF16 ? 8 : 4; }
 //   to be joined (us, one row of 50257 bf16, in 1 / 8 parts: without alternatives 5.2 / 4.2, with 100 12.7 / 14);
 //   where alternatives are wanted of many or of long rows, so that more workgroups of fewer waves share a compute unit
 //   and one's search runs under another's loads (2048 rows of 50257 fp32, in 1 / 4 parts: with 20 105 / 84, with 64 127 /
-//   114, with 100 142 / 140; 4096 rows of bf16, in 1 / 2: with 20 121 / 102, with 64 140 / 140; 200 rows of 250007 bf16, in
+//   104, with 100 131 / 121; 4096 rows of bf16, in 1 / 2: with 20 121 / 102, with 64 140 / 140; 200 rows of 250007 bf16, in
 //   2 / 8: with 20 37 / 28, in 2 / 4: with 100 47 / 41).
 // The distillation's list is read in every workgroup of a row that is not cut, and in a launch of its own where it is: rows that
 // fit eight vectors a thread are not (loss and gradient of 24 rows of 50257 bf16, in 1 / 8 parts 9.2 / 11).
@@ -1149,7 +1197,7 @@ Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most, int most_nv,
     const int64_t useful = (vectors + 511) / 512;
     if (splits > useful) splits = useful;
     if (k > 0 && (least > 1 || (T >= 512 && vectors > 8 * most) || (T >= 2048 && k <= 32))) {
-        const int64_t part = k <= 64 ? kSmall : 8 * most;
+        const int64_t part = k <= 64 || dtype == BCQ_F32 ? kSmall : 8 * most;
         splits = (vectors + part - 1) / part;
     }
     if (splits > bcq::LG_MAX_SPLITS) splits = bcq::LG_MAX_SPLITS;
@@ -1166,7 +1214,10 @@ Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most, int most_nv,
     else if (p.per <= (few ? 4 * most : 1536)) p.nv = 4;
     else p.nv = p.per <= 8 * most ? 8 : p.per <= 16 * most ? 16 : most_nv;
     p.threads = ((p.per + p.nv - 1) / p.nv + 63) / 64 * 64;
-    if (p.threads < 256) p.threads = 256;
+    // the least: what the barriers of a search need no longer wait for (us, 16384 rows of 1000 bf16 at 64 / 128 / 256 threads: no
+    // alternatives 9.7 / 12.6 / 22, with 5 35 / 35 / 45, with 64 57 / 49 / 62)
+    const int fewest = k > 0 ? 128 : 64;
+    if (p.threads < fewest) p.threads = fewest;
     return p;
 }
 Plan logprobs_plan(int64_t T, int64_t V, int dtype, int k) { return forward_plan(T, V, dtype, k, bcq::LG_MAX_THREADS, bcq::LG_MAX_NV, false); }
@@ -1197,21 +1248,31 @@ void slices(int64_t T, int64_t threads_per_row, F f) {
     for (int64_t t = 0; t < T; t += rows) f(t, (unsigned)(T - t < rows ? T - t : rows));
 }
 
-template <typename XT, int NV, bool ENT, bool TOP>
+template <typename XT, int NV, bool ENT, bcq::LogprobsTop TOP>
 void launch_logprobs_as(bcq::LogprobsArgs a, int64_t T, int threads, hipStream_t st) {
+    constexpr bool kTop = TOP != bcq::LG_NO_TOP;
     slices(T, (int64_t)a.splits * threads, [&](int64_t row0, unsigned rows) {
         a.row0 = row0;
         BCQ_LAUNCH((bcq::logprobs_kernel<XT, NV, ENT, TOP>), dim3(rows * a.splits), dim3(threads), 0, st, a);
-        if (a.splits > 1) BCQ_LAUNCH((bcq::logprobs_join_kernel<XT, ENT, TOP>), dim3(rows), dim3(TOP ? 256 : 64), 0, st, a);
+        if (a.splits > 1) BCQ_LAUNCH((bcq::logprobs_join_kernel<XT, ENT, kTop>), dim3(rows), dim3(kTop ? 256 : 64), 0, st, a);
     });
+}
+template <typename XT, int NV, bool ENT>
+void launch_logprobs_top(const bcq::LogprobsArgs& a, int64_t T, int threads, hipStream_t st) {
+    // LG_DIRECT costs an instruction or a few for every entry of a thread (bf16 has to be unpacked, twice), LG_STAGED a turn for every
+    // four threads of a wave that hold candidates: by the entries of a chunk to each alternative wanted.  (us, staged / direct:
+    // fp32, 2048 rows of 50257 in 4 chunks with 20, 40, 64 alternatives 83 / 86, 94 / 94, 112 / 103, 16384 rows of 1000 with 5, 64
+    // 39 / 36, 95 / 55; bf16, 16384 rows of 8192 with 20, 40, 64 64 / 78, 80 / 86, 110 / 102, of 4000 with 20, 40 59 / 60, 75 / 64.)
+    const int64_t entries = (int64_t)a.per * bcq::LgVec<XT>::N;
+    const bool direct = a.k * (sizeof(XT) == 2 ? 192 : 512) >= entries;
+    if (!a.k) launch_logprobs_as<XT, NV, ENT, bcq::LG_NO_TOP>(a, T, threads, st);
+    else if (direct) launch_logprobs_as<XT, NV, ENT, bcq::LG_DIRECT>(a, T, threads, st);
+    else launch_logprobs_as<XT, NV, ENT, bcq::LG_STAGED>(a, T, threads, st);
 }
 template <typename XT, int NV>
 void launch_logprobs_nv(const bcq::LogprobsArgs& a, int64_t T, int threads, hipStream_t st) {
-    if (a.entropy) {
-        if (a.k) launch_logprobs_as<XT, NV, true, true>(a, T, threads, st);
-        else launch_logprobs_as<XT, NV, true, false>(a, T, threads, st);
-    } else if (a.k) launch_logprobs_as<XT, NV, false, true>(a, T, threads, st);
-    else launch_logprobs_as<XT, NV, false, false>(a, T, threads, st);
+    if (a.entropy) launch_logprobs_top<XT, NV, true>(a, T, threads, st);
+    else launch_logprobs_top<XT, NV, false>(a, T, threads, st);
 }
 template <typename XT>
 hipError_t launch_logprobs(const bcq::LogprobsArgs& a, int64_t T, const Plan& p, hipStream_t st) {

@@ -348,6 +348,18 @@ def test_top_of_ties_and_orders(pattern, V, dtype):
         assert torch.isnan(out.top_logp).all() == (pattern == "nan")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(40, 100), (40, 515), (40, 1000), (40, 4000), (17, 18610), (600, 8192), (520, 40003), (5, 60000)])
+def test_top_of_every_size(T, V, dtype):
+    """Rows of few and many entries to an alternative, whole and in parts."""
+    x = table(T, V, dtype, seed=V + 1)
+    order = best(x, min(V, 128))
+    for k in (1, 3, 20, 33, 64, 100, 128):
+        out = bcq.bcq_logprobs_fwd(x, k=k)
+        assert torch.equal(out.top_index.cpu()[:, :V], order[:, :k])
+        assert (out.top_index[:, V:] == -1).all() and torch.isneginf(out.top_logit[:, V:]).all()
+
+
 def test_tokens_out_of_range_and_skipped_rows():
     T, V = 5, 3001
     x = table(T, V, "bf16")
