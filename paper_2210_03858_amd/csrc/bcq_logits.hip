@@ -1229,15 +1229,17 @@ Plan distill_plan(int64_t T, int64_t V, int dtype, bool gradient) {
     const int nv = gradient && vectors <= bcq::LG_MAX_NV_GRADIENT * most ? bcq::LG_MAX_NV_GRADIENT : bcq::LG_MAX_NV;
     return forward_plan(T, V, dtype, 0, most, nv, true);
 }
-// For the gradients from saved statistics: nothing is joined, so chunks are small.
+// For the gradients from saved statistics: nothing is joined, so chunks are small; short rows get as few threads as
+// hold them, `fewest` at least (16384 rows of 1000 bf16, with 256 / 64 threads 24 / 14 us).
 constexpr int kBwdNv = 4;
-Plan backward_plan(int64_t V, int dtype) {
+Plan backward_plan(int64_t V, int dtype, int fewest) {
     const int64_t vectors = (V + vector_entries(dtype) - 1) / vector_entries(dtype);
     Plan p;
     p.nv = kBwdNv;
-    p.threads = 256;
-    p.splits = (int)((vectors + kBwdNv * 256 - 1) / (kBwdNv * 256));
-    p.per = kBwdNv * 256;
+    const int64_t threads = (vectors + kBwdNv - 1) / kBwdNv;
+    p.threads = threads >= 256 ? 256 : threads <= fewest ? fewest : (int)((threads + 63) / 64 * 64);
+    p.per = kBwdNv * p.threads;
+    p.splits = vectors <= p.per ? 1 : (int)((vectors + p.per - 1) / p.per);
     return p;
 }
 
@@ -1417,7 +1419,7 @@ bcq_status bcq_logprobs_bwd(const void* logits, int dtype, int64_t T, int64_t V,
         return BCQ_ERR_ALIGN;
     if (!bcq::host::device_ok()) return BCQ_ERR_DEVICE;
     if (T == 0) return BCQ_OK;
-    const Plan p = backward_plan(V, dtype);
+    const Plan p = backward_plan(V, dtype, 64);
     const bcq::LogprobsBwdArgs a{logits, row_stride, tokens, stats, dlogp, entropy, dentropy, 1.0f / temperature, (int)V, p.splits,
                                  p.per, 0, dlogits, grad_stride};
     hipStream_t st = (hipStream_t)stream;
@@ -1468,7 +1470,7 @@ hipError_t run_distill(bcq::DistillArgs d, const DistillCall& a, const Plan& p, 
     return a.dtype == BCQ_BF16 ? launch_distill<bcq::bf16_t, MODE>(d, a.T, p, st) : launch_distill<float, MODE>(d, a.T, p, st);
 }
 hipError_t run_distill_bwd(const bcq::DistillArgs& d, const DistillCall& a, hipStream_t st) {
-    const Plan p = backward_plan(a.V, a.dtype);
+    const Plan p = backward_plan(a.V, a.dtype, BCQ_LOGITS_MAX_K);
     return a.dtype == BCQ_BF16 ? launch_distill_bwd<bcq::bf16_t>(d, a.T, p, st) : launch_distill_bwd<float>(d, a.T, p, st);
 }
 
