@@ -48,6 +48,9 @@ __device__ __forceinline__ uint64_t lg_entry(float v, int index) { return ((uint
 // what the lanes of a wave wrote to LDS is there for its other lanes
 __device__ __forceinline__ void lg_wave_sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
+// a value that is the same in all lanes, as such
+__device__ __forceinline__ uint32_t lg_uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // ---- reductions: over the 16 lanes of a row, and over a wave; every lane gets the result
 template <int CTRL>
 __device__ __forceinline__ float lg_move(float v) { return __uint_as_float(dpp_move<CTRL>(__float_as_uint(v))); }
@@ -460,7 +463,7 @@ __device__ __forceinline__ void lg_bound(L& lds, int k) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) key[u] = lg_key(group[u]);
     const float most = lg_max2(lg_max2(group[0], group[1]), lg_max2(group[2], group[3]));
-    const uint32_t high = lg_key(lg_wave_max(most)) + 1;
+    const uint32_t high = lg_uniform(lg_key(lg_wave_max(most)) + 1);
     auto reached = [&](uint32_t at) {
         uint32_t c = (uint32_t)__popcll(__ballot(key[0] >= at));
         if (k > 32) c += (uint32_t)__popcll(__ballot(key[1] >= at));
@@ -496,7 +499,7 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV, TOP>& lds, LgChunk<XT, N
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     if (wave == 0) lg_bound(lds, k);
     __syncthreads();
-    uint32_t low = lds.low, high = lds.high;
+    uint32_t low = lg_uniform(lds.low), high = lg_uniform(lds.high);
     // A bound as low as a mask's value: the masked entries are many, so only those above are taken, and as many of the masked
     // as are missing then looked for in order.
     const bool masks = lg_unkey(low) < -0x1p100f;
@@ -585,7 +588,7 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV, TOP>& lds, LgChunk<XT, N
         }
     }
     __syncthreads();
-    int n = lds.n;
+    int n = (int)lg_uniform(lds.n);
     float value;  // n entries are above it, fewer than k; the others equal it
     if (n <= LG_CANDIDATES) {
         if (!masks || n >= k) return n;
@@ -652,7 +655,7 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV, TOP>& lds, LgChunk<XT, N
         if (lane == 0) lds.n = at < k ? at : k;
     }
     __syncthreads();
-    return lds.n;
+    return (int)lg_uniform(lds.n);
 }
 
 // One pass over the chunk in registers for maximum and sums, then the search for alternatives.  Without alternatives the
@@ -746,7 +749,7 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobsArgs a) {
             if (entry >= bound) list[atomicAdd(&count, 1)] = entry;
         }
         __syncthreads();
-        lg_rank(list, count, a.k, [&](int rank, uint64_t entry) { lg_write_top(a, t, rank, entry, p, l2); });
+        lg_rank(list, (int)lg_uniform(count), a.k, [&](int rank, uint64_t entry) { lg_write_top(a, t, rank, entry, p, l2); });
     }
 }
 
