@@ -75,6 +75,14 @@ __device__ __forceinline__ float lg_wave_sum(float v) {
     v = lg_row_sum(v);
     return (lg_lane(v, 0) + lg_lane(v, 16)) + (lg_lane(v, 32) + lg_lane(v, 48));
 }
+__device__ __forceinline__ uint32_t lg_wave_min(uint32_t v) {
+    v = min(v, dpp_move<DPP_XOR1>(v));
+    v = min(v, dpp_move<DPP_XOR2>(v));
+    v = min(v, dpp_move<DPP_HALF_MIRROR>(v));
+    v = min(v, dpp_move<DPP_MIRROR>(v));
+    auto lane = [&](int l) { return (uint32_t)__builtin_amdgcn_readlane(v, l); };
+    return min(min(lane(0), lane(16)), min(lane(32), lane(48)));
+}
 
 // Sums of a part of a row: S = sum 2^d, E = sum 2^d d, d = (x - m) c2.  m is the part's maximum or a value near it: S lies
 // between 2^-32 and 2^32 or so; -inf where the part holds nothing.
@@ -733,15 +741,11 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobsArgs a) {
     const float l2 = __builtin_amdgcn_logf(p.S);
     if (tid == 0) lg_write_row<XT>(a, t, token, p, l2);
     if constexpr (TOP) {
-        // The first ceil(k / splits) entries of every list are k together: the least of their last ones is a lower bound.
+        // The first ceil(k / splits) entries of every list are k together: the least value of their last ones is a lower bound.
         const uint64_t* lists = a.lists + t * a.splits * a.k;
         const int deep = (a.k + a.splits - 1) / a.splits;
-        uint64_t bound = lane < a.splits ? lists[lane * a.k + deep - 1] : ~(uint64_t)0;
-        for (int s = 1; s < 64; s *= 2) {
-            const uint64_t other = __shfl_xor((unsigned long long)bound, s);
-            bound = other < bound ? other : bound;
-        }
-        if (bound == 0) bound = 1;  // entries that are missing
+        const uint32_t least = lg_wave_min(lane < a.splits ? (uint32_t)(lists[lane * a.k + deep - 1] >> 32) : UINT_MAX);
+        const uint64_t bound = least ? (uint64_t)least << 32 : 1;  // 0: entries that are missing
         if (tid == 0) count = 0;
         __syncthreads();
         for (int i = tid; i < a.splits * a.k; i += 256) {
