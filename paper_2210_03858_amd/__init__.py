@@ -1,6 +1,8 @@
 """MI355X-native BCQ linear layer (AlphaTuning, arXiv 2210.03858): HIP kernels behind a C ABI.
 
-`binding` holds the thin ctypes layer over libbcq_hip.so; `synth` holds the seeded input generators.
+`binding` holds the thin ctypes layer over libbcq_hip.so, `autograd` the differentiable forms; `synth` holds the seeded input
+generators.  Beside the layer stand the operators on logits that its training and answers end in: log probabilities with entropy
+and alternatives, and distillation from a teacher's top logits.
 """
 from . import synth  # noqa: F401
 from .binding import (BatchPlan, BcqError, batch_plan, bcq_batch_prepare, bcq_linear_batched, bcq_prepare, abi_version, bcq_alpha_adamw_step, bcq_linear_bwd_alpha_adamw, bcq_linear_bwd_alpha, bcq_linear_bwd_alpha_grouped,  # noqa: F401

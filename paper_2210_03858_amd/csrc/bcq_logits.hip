@@ -37,7 +37,7 @@ __device__ __forceinline__ float lg_max2(float a, float b) { return lg_max3(a, b
 // A float as an unsigned number of the same order (-0 as +0); 0 is below every number.  NaN is not passed in.
 __device__ __forceinline__ uint32_t lg_key(float v) {
     const uint32_t u = __float_as_uint(v + 0.0f);
-    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float lg_unkey(uint32_t key) {
     return __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
@@ -542,6 +542,7 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV, TOP>& lds, LgChunk<XT, N
                 for (int e = 0; e < N; ++e) {
                     const float x = LgVec<XT>::get(chunk.w[i], e);
                     const uint64_t these = __ballot(x >= bound);
+                    if (these == 0) continue;
                     const int here = at + __popcll(these & below);
                     if (x >= bound && here < LG_CANDIDATES)
                         lds.list[here] = lg_entry(x, chunk.head + (chunk.first + chunk.place_of(i)) * N + e);
