@@ -195,6 +195,8 @@ struct LgChunk {
     __device__ __forceinline__ void load(const XT* row, int threads_) {
         const int tid = threadIdx.x;
         threads = threads_;
+        // first: loads return in order, and a sum begins with it
+        edge = edge_index >= 0 ? Elem<XT>::load(row + edge_index) : -INFINITY;
         if (n > 0) {
             const char* base = reinterpret_cast<const char*>(row + head) + (int64_t)first * 16;
 #pragma unroll
@@ -204,7 +206,6 @@ struct LgChunk {
                 w[i][0] = q.x, w[i][1] = q.y, w[i][2] = q.z, w[i][3] = q.w;
             }
         }
-        edge = edge_index >= 0 ? Elem<XT>::load(row + edge_index) : -INFINITY;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if ((i + 1) * threads > n && i * threads + tid >= n) w[i][0] = w[i][1] = w[i][2] = w[i][3] = Vec::NONE;
