@@ -1191,24 +1191,26 @@ int vector_entries(int dtype) { return dtype == BCQ_BF16 ? 8 : 4; }
 // workgroup's registers, and
 //   where fewer than 64 are there, to spread them over the card, unless alternatives are wanted, whose lists would have
 //   to be joined (us, one row of 50257 bf16, in 1 / 8 parts: without alternatives 5.2 / 4.2, with 100 12.7 / 14);
-//   where alternatives are wanted of many or of long rows, so that more workgroups of fewer waves share a compute unit
-//   and one's search runs under another's loads (2048 rows of 50257 fp32, in 1 / 4 parts: with 20 105 / 84, with 64 127 /
-//   104, with 100 131 / 121; 4096 rows of bf16, in 1 / 2: with 20 121 / 102, with 64 140 / 140; 200 rows of 250007 bf16, in
-//   2 / 8: with 20 37 / 28, in 2 / 4: with 100 47 / 41).
+//   where alternatives are wanted of long rows, into chunks of eight waves, of which four share a compute unit so that one's
+//   search runs under another's loads (2048 rows of 50257 fp32, in 1 / 4 parts: with 20 105 / 81, with 64 115 / 96, with
+//   100 122 / 113; 1000 rows of 128001 bf16, in 2 / 4 / 5: with 20 51 / 49 / 60, with 64 63 / 66 / 84; 800 rows of 150000, in
+//   3 / 5: with 100 94 / 73; 300 rows of 128001 fp32, in 4 / 8 / 9: with 20 32 / 31 / 34);
+//   where alternatives are wanted of many rows whose 11 to 15 waves would leave a third of a compute unit's 32 empty (4096
+//   rows of 50257 bf16, in 1 / 2 parts: with 20 117 / 99, with 40 130 / 115, with 64 135 / 137; with 9 or 16 waves not: 2100
+//   rows of 36000 bf16 with 20 37 / 44, of 32003 fp32 44 / 48).
 // The distillation's list is read in every workgroup of a row that is not cut, and in a launch of its own where it is: rows that
 // fit eight vectors a thread are not (loss and gradient of 24 rows of 50257 bf16, in 1 / 8 parts 9.2 / 11).
 Plan forward_plan(int64_t T, int64_t V, int dtype, int k, int most, int most_nv, bool listed) {
-    constexpr int64_t kSmall = 7 * 64 * 8;  // vectors of a workgroup of seven waves
+    constexpr int64_t kSmall = 8 * 512;  // vectors of a workgroup of eight waves
     const int64_t vectors = (V + vector_entries(dtype) - 1) / vector_entries(dtype);
     const int64_t least = (vectors + most_nv * most - 1) / (most_nv * most);
     const bool one = least == 1 && (T >= 64 || k > 0 || (listed && vectors <= 8 * most));
     int64_t splits = one ? 1 : (512 + T - 1) / (T > 0 ? T : 1);
     const int64_t useful = (vectors + 511) / 512;
     if (splits > useful) splits = useful;
-    if (k > 0 && (least > 1 || (T >= 512 && vectors > 8 * most) || (T >= 2048 && k <= 32))) {
-        const int64_t part = k <= 64 || dtype == BCQ_F32 ? kSmall : 8 * most;
-        splits = (vectors + part - 1) / part;
-    }
+    const bool gap = vectors > 10 * 512 && vectors <= 15 * 512;
+    if (k > 0 && (least > 1 || (T >= 512 && vectors > 8 * most) || (T >= 2048 && k <= 48 && gap)))
+        splits = (vectors + kSmall - 1) / kSmall;
     if (splits > bcq::LG_MAX_SPLITS) splits = bcq::LG_MAX_SPLITS;
     if (k > 0 && splits * k > bcq::LG_JOIN_CANDIDATES) splits = bcq::LG_JOIN_CANDIDATES / k;
     if (splits < least) splits = least;
@@ -1270,12 +1272,13 @@ void launch_logprobs_as(bcq::LogprobsArgs a, int64_t T, int threads, hipStream_t
 }
 template <typename XT, int NV, bool ENT>
 void launch_logprobs_top(const bcq::LogprobsArgs& a, int64_t T, int threads, hipStream_t st) {
-    // LG_DIRECT costs an instruction or a few for every entry of a thread (bf16 has to be unpacked, twice), LG_STAGED a turn for every
+    // LG_DIRECT costs an instruction or two for every entry of a thread (bf16 has to be unpacked, twice), LG_STAGED a turn for every
     // four threads of a wave that hold candidates: by the entries of a chunk to each alternative wanted.  (us, staged / direct:
-    // fp32, 2048 rows of 50257 in 4 chunks with 20, 40, 64 alternatives 83 / 86, 94 / 94, 112 / 103, 16384 rows of 1000 with 5, 64
-    // 39 / 36, 95 / 55; bf16, 16384 rows of 8192 with 20, 40, 64 64 / 78, 80 / 86, 110 / 102, of 4000 with 20, 40 59 / 60, 75 / 64.)
+    // fp32, 2048 rows of 50257 in 4 chunks with 5, 20, 64 alternatives 73 / 74, 82 / 81, 111 / 96, 16384 rows of 1000 with 1, 64
+    // 30 / 25, 96 / 48; bf16, 4096 rows of 50257 in 2 chunks with 20, 64, 100 98 / 105, 136 / 137, 146 / 142, 16384 rows of 8192 with
+    // 20, 40 69 / 71, 84 / 79, of 4000 with 5, 40 40 / 39, 77 / 58.)
     const int64_t entries = (int64_t)a.per * bcq::LgVec<XT>::N;
-    const bool direct = a.k * (sizeof(XT) == 2 ? 192 : 512) >= entries;
+    const bool direct = a.k * (sizeof(XT) == 2 ? 384 : 1024) >= entries;
     if (!a.k) launch_logprobs_as<XT, NV, ENT, bcq::LG_NO_TOP>(a, T, threads, st);
     else if (direct) launch_logprobs_as<XT, NV, ENT, bcq::LG_DIRECT>(a, T, threads, st);
     else launch_logprobs_as<XT, NV, ENT, bcq::LG_STAGED>(a, T, threads, st);
