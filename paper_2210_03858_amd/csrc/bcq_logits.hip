@@ -669,11 +669,11 @@ __device__ __forceinline__ int lg_candidates(TopLds<NV, TOP>& lds, LgChunk<XT, N
 }
 
 // One pass over the chunk in registers for maximum and sums, then the search for alternatives.  Without alternatives the
-// reading of the logits bounds it: 4096 rows of 50257 bf16 in 70 us, 5.9 TB/s.  With them it is the search, a chain of short
-// steps between barriers, as far as it does not run under the loads of the other workgroups of its compute unit: 2048 rows of
-// 50257 fp32 with 64 alternatives in 115 us, 3.6 TB/s.  So residency counts.  Eight waves a SIMD need at most 64 vector and
-// 80 scalar registers each (the compiler by itself takes 96 of these), which the attributes ask for; sixteen vectors a
-// thread do not fit that and get the registers of four waves.
+// reading of the logits bounds it: 4096 rows of 50257 bf16 in 71 us, 5.8 TB/s.  With them it is vector instructions and the
+// search's chain of short steps between barriers, as far as those do not run under the loads of the other workgroups of the
+// compute unit: 2048 rows of 50257 fp32 with 64 alternatives in 98 us, 4.2 TB/s.  So residency counts.  Eight waves a SIMD
+// need at most 64 vector and 80 scalar registers each (the compiler by itself takes 96 of these), which the attributes ask
+// for; sixteen vectors a thread do not fit that and get the registers of four waves.
 template <typename XT, int NV, bool ENT, LogprobsTop TOP>
 __global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80), amdgpu_waves_per_eu(NV <= 8 ? 7 : 4))) void logprobs_kernel(LogprobsArgs a) {
     __shared__ Part parts[16];
@@ -1029,7 +1029,7 @@ struct LgBits {
 enum DistillMode { LG_SUMS, LG_LOSS, LG_GRADIENT };
 // With the gradient the row is read once and written once, which bounds it: 16384 rows of 50257 bf16 with 64 listed in 647 us,
 // 5.1 TB/s.  For the loss alone it is the list, whose two dependent loads and 64-bit exponentials and logarithms end after the
-// row's own loads: 420 us with the list as the whole teacher 304, 3.9 and 5.4 TB/s.  (Exponentials in 32 bits would be faster;
+// row's own loads: 425 us with a rest and 304 without, 3.9 and 5.4 TB/s.  (Exponentials in 32 bits would be faster;
 // the rest 1 - sum p of a list that holds nearly all of the teacher's probability would then be rounding error.)
 template <typename XT, int NV, bool REST, DistillMode MODE>
 __global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80))) void distill_kernel(DistillArgs a) {
@@ -1122,7 +1122,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a) {
     }
 }
 
-// As the other gradient: 16384 rows of 50257 bf16 in 620 us, 5.3 TB/s.
+// As the other gradient, bound by its traffic: 16384 rows of 50257 bf16 in 618 us, 5.3 TB/s.
 template <typename XT, int NV, bool REST>
 __global__ __launch_bounds__(256) void distill_bwd_kernel(DistillArgs a) {
     __shared__ alignas(16) int index[BCQ_LOGITS_MAX_K];
