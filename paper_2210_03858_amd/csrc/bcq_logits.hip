@@ -885,13 +885,21 @@ __device__ __forceinline__ void lg_load_list(ListLds& L, const DistillArgs& a, i
             }
         lg_wave_sync();
     }
+    // p relative to the teacher's log sum, or to the list's maximum first and its sum then
     double norm;
-    if constexpr (REST) {
-        norm = (double)a.teacher_lse[t];
-    } else {
-        const double top = (double)lg_shift(lg_wave_max(lg_max2((float)lp[0], (float)lp[1])));
-        const double sum = wave_sum(exp(lp[0] - top) + exp(lp[1] - top));
-        norm = sum == 0.0 ? 0.0 : top + log(sum);
+    if constexpr (REST) norm = (double)a.teacher_lse[t];
+    else norm = (double)lg_shift(lg_wave_max(lg_max2((float)lp[0], (float)lp[1])));
+    p[0] = exp(lp[0] - norm);
+    p[1] = a.k > 64 ? exp(lp[1] - norm) : 0.0;
+    if constexpr (!REST) {
+        const double sum = wave_sum(p[0] + p[1]);
+        if (sum == 0.0) {
+            norm = 0.0;
+        } else {
+            norm += log(sum);
+            p[0] /= sum;
+            p[1] /= sum;
+        }
     }
     double P = 0.0, H = 0.0, U = 0.0;
     const float m = lg_wave_max(lg_max2(s[0], s[1])), shift = lg_shift(m);
@@ -899,7 +907,6 @@ __device__ __forceinline__ void lg_load_list(ListLds& L, const DistillArgs& a, i
     bool bad = false;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        p[u] = exp(lp[u] - norm);
         P += p[u];
         if (p[u] != 0.0) {
             H += p[u] * (lp[u] - norm);
@@ -972,12 +979,21 @@ __device__ __forceinline__ DistillStats lg_distill_stats(const ListLds& L, Part 
     }
     return d;
 }
-// the row's loss, in 64 bits
+// the row's loss, in 64 bits, by a whole wave: its three logarithms in three lanes
 __device__ __forceinline__ float lg_distill_loss(const ListLds& L, Part u, const DistillStats& d, float S, float c, bool rest, int V) {
-    const double lS = S == 0.f ? 0.0 : log((double)S), r = lg_rest(L, rest, V);
+    const double r = lg_rest(L, rest, V);
+    const int lane = threadIdx.x & 63;
+    const double of[3] = {(double)S, r, (double)u.S};
+    const double l = log(lane == 0 ? of[0] : lane == 1 ? of[1] : of[2]);
+    auto log_of = [&](int i) {
+        const uint64_t w = (uint64_t)__double_as_longlong(l);
+        const uint32_t low = __builtin_amdgcn_readlane((uint32_t)w, i), high = __builtin_amdgcn_readlane((uint32_t)(w >> 32), i);
+        return __longlong_as_double((long long)(((uint64_t)high << 32) | low));
+    };
+    const double lS = S == 0.f ? 0.0 : log_of(0), lr = log_of(1), lu = log_of(2);
     double value = L.H;
     if (L.P != 0.0) value -= L.U + L.P * ((double)(lg_shift(L.m) - d.m_all) * c - lS);
-    if (rest && r != 0.0) value += r * (log(r) - (log((double)u.S) + (double)(d.m - d.m_all) * c - lS));
+    if (rest && r != 0.0) value += r * (lr - (lu + (double)(d.m - d.m_all) * c - lS));
     if (L.distinct == 0) return 0.f;
     return L.bad ? NAN : (float)(value / ((double)c * c));
 }
@@ -1083,8 +1099,9 @@ __global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80))
         float S;
         const DistillStats d = lg_distill_stats(L, p, a.c, REST, a.V, S);
         if (tid >= (int)blockDim.x - 64) {
+            const float loss = lg_distill_loss(L, p, d, S, a.c, REST, a.V);
             if ((tid & 63) == 0) {
-                a.loss[t] = lg_distill_loss(L, p, d, S, a.c, REST, a.V);
+                a.loss[t] = loss;
                 if constexpr (MODE == LG_LOSS) lg_write_distill(a, t, d, (float)L.norm);
             }
         } else if constexpr (MODE == LG_GRADIENT) {
@@ -1114,10 +1131,11 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a) {
     __syncthreads();
     const float4 f = lane < a.splits ? a.parts[t * a.splits + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
     const Part p = lg_wave_join<false>(Part{f.x, f.y, 0.f}, a.c * LG_LOG2E);
+    float S;
+    const DistillStats d = lg_distill_stats(L, p, a.c, REST, a.V, S);
+    const float loss = lg_distill_loss(L, p, d, S, a.c, REST, a.V);
     if (lane == 0) {
-        float S;
-        const DistillStats d = lg_distill_stats(L, p, a.c, REST, a.V, S);
-        a.loss[t] = lg_distill_loss(L, p, d, S, a.c, REST, a.V);
+        a.loss[t] = loss;
         lg_write_distill(a, t, d, (float)L.norm);
     }
 }
