@@ -1045,7 +1045,7 @@ struct LgBits {
 enum DistillMode { LG_SUMS, LG_LOSS, LG_GRADIENT };
 // With the gradient the row is read once and written once, which bounds it: 16384 rows of 50257 bf16 with 64 listed in 647 us,
 // 5.1 TB/s.  For the loss alone it is the list, whose two dependent loads and 64-bit exponentials and logarithms end after the
-// row's own loads: 425 us with a rest and 304 without, 3.9 and 5.4 TB/s.  (Exponentials in 32 bits would be faster;
+// row's own loads: 424 us with a rest and 285 without, 3.9 and 5.8 TB/s.  (Exponentials in 32 bits would be faster;
 // the rest 1 - sum p of a list that holds nearly all of the teacher's probability would then be rounding error.)
 template <typename XT, int NV, bool REST, DistillMode MODE>
 __global__ __launch_bounds__(LG_MAX_THREADS) __attribute__((amdgpu_num_sgpr(80))) void distill_kernel(DistillArgs a) {

@@ -551,3 +551,35 @@ def test_refusals():
     assert bcq.bcq_logprobs_fwd(empty, tok[:0], k=2).top_index.shape == (0, 2)
     loss, dx = bcq.bcq_distill_fwd_bwd(empty, z[:0], j[:0])
     assert loss.shape == (0,) and dx.shape == (0, 100)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_autograd_of_nothing_and_of_other_shapes(native, monkeypatch):
+    """No rows; tables of more dimensions; rows whose entries are not next to each other; a gradient that is one number for all."""
+    if not native:
+        monkeypatch.setattr(autograd.B, "_try_native", lambda *a: None)
+    none = torch.zeros((0, 40), device="cuda", requires_grad=True)
+    logp, _ = autograd.token_logprobs(none, torch.zeros((0,), dtype=torch.int64, device="cuda"))
+    loss = autograd.distill_loss(none, torch.zeros((0, 3), device="cuda"), torch.zeros((0, 3), dtype=torch.int32, device="cuda"))
+    (logp.sum() + loss.sum()).backward()
+    assert logp.shape == loss.shape == (0,) and none.grad.shape == (0, 40)
+
+    gen = torch.Generator().manual_seed(7)
+    x = torch.randn((3, 5, 77), generator=gen, dtype=torch.float64)
+    tok = torch.randint(77, (3, 5), generator=gen)
+    z, j = torch.randn((3, 5, 4), generator=gen), torch.randint(77, (3, 5, 4), generator=gen)
+    for layout in (lambda v: v, lambda v: v.transpose(1, 2).contiguous().transpose(1, 2)):
+        a = layout(x.float().cuda()).requires_grad_()
+        logp, H = autograd.token_logprobs(a, tok.cuda(), entropy=True)
+        loss = autograd.distill_loss(a, z.cuda(), j.int().cuda())
+        (logp.sum() + H.sum() + loss.sum()).backward()
+        b = x.float().double().requires_grad_()
+        logq = torch.log_softmax(b, -1)
+        p = torch.softmax(z.double(), -1)
+        ref = (logq.gather(-1, tok[..., None])[..., 0], -(logq.exp() * logq).sum(-1),
+               (p * (p.log() - logq.gather(-1, j))).sum(-1))
+        sum(r.sum() for r in ref).backward()
+        for got, want in zip((logp, H, loss), ref):
+            assert got.shape == (3, 5)
+            close(got.detach().reshape(-1), want.detach().reshape(-1).cuda())
+        assert (a.grad.double().cpu() - b.grad).abs().max() < GRAD * 8
