@@ -583,3 +583,24 @@ def test_autograd_of_nothing_and_of_other_shapes(native, monkeypatch):
             assert got.shape == (3, 5)
             close(got.detach().reshape(-1), want.detach().reshape(-1).cuda())
         assert (a.grad.double().cpu() - b.grad).abs().max() < GRAD * 8
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(6, 700), (6, 12007), (530, 40003), (6, 140001)])
+def test_many_alternatives_of_masked_rows(T, V, dtype):
+    """More alternatives than a row has entries beside its mask, about as many, and NaN among them."""
+    for mask in (-INF, torch.finfo(DTYPES[dtype]).min, -1e9):
+        x = table(T, V, dtype, seed=V)
+        gen = torch.Generator().manual_seed(5)
+        for row, left in enumerate((0, 1, 60, 100, 300)):
+            keep = torch.randperm(V, generator=gen)[:left]
+            masked = torch.full((V,), mask, dtype=x.dtype)
+            masked[keep] = x[row].cpu()[keep]
+            x[row] = masked.cuda()
+        x[3, V // 3] = float("nan")
+        for k in (70, 128):
+            out = bcq.bcq_logprobs_fwd(x, k=k)
+            index = best(x, k)
+            assert torch.equal(out.top_index.cpu(), index), (mask, k)
+            want = torch.where(index < 0, -INF, x.float().cpu().gather(1, index.long().clamp(min=0)))
+            assert torch.equal(out.top_logit.cpu(), want)
